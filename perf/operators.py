@@ -9,8 +9,8 @@ Kinds:
   swiglu    a = g sigmoid(g) u forward (serving)
   swiglu_train
             the same forward writing 8-bit checkpoints of g and u, then the
-            backward from them: dg, du and a once more (the down projection's
-            input in its own backward)
+            backward's part from them: a once more (the down projection's
+            input, for its adapter's gradient), and dg and du
   swiglu_bwd
             the backward from g and u as they are
   combine   a token's expert outputs summed with the router weights
@@ -224,7 +224,8 @@ def _run_own(s):
         return ace.ace_swiglu_fwd(s["g"], s["u"], s["a"])
     if kind == "swiglu_train":
         ace.ace_swiglu_fwd(s["g"], s["u"], s["a"], g_packed=s["g8"], u_packed=s["u8"])
-        ace.ace_swiglu_bwd(s["da"], s["g8"], s["u8"], s["dg"], s["du"], a=s["a_again"])
+        ace.ace_swiglu_fwd(s["g8"], s["u8"], s["a_again"])
+        ace.ace_swiglu_bwd(s["da"], s["g8"], s["u8"], s["dg"], s["du"])
         return {"a": s["a"], "a_again": s["a_again"], "dg": s["dg"], "du": s["du"]}
     if kind == "swiglu_bwd":
         ace.ace_swiglu_bwd(s["da"], s["g"], s["u"], s["dg"], s["du"])
@@ -406,5 +407,5 @@ def work(case):
         return {"bytes": 3 * b * n * d, "flops": 5 * n * d}
     if kind == "swiglu_bwd":
         return {"bytes": 5 * b * n * d, "flops": 12 * n * d}
-    # forward: g, u -> a and two checkpoints; backward: da, checkpoints -> dg, du, a
-    return {"bytes": 7 * b * n * d + 4 * packed, "flops": 30 * n * d}
+    # g, u -> a and two checkpoints; these -> a; these and da -> dg, du
+    return {"bytes": 7 * b * n * d + 6 * packed, "flops": 30 * n * d}
