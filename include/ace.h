@@ -97,7 +97,8 @@ typedef enum {
   ACE_OP_PERMUTE = 0,
   ACE_OP_FWD = 1,
   ACE_OP_BWD = 2,
-  ACE_OP_CKA = 3   /* ace_pairwise_cka: T = probe rows N, k = 1, n_keys = E, r_max = rank */
+  ACE_OP_CKA = 3,  /* ace_pairwise_cka: T = probe rows N, k = 1, n_keys = E, r_max = rank */
+  ACE_OP_MOE_DX = 4 /* ace_moe_dx: n_keys = E, r_max ignored                     */
 } ace_op;
 
 /*
@@ -309,6 +310,115 @@ ace_status ace_moe_lora_fwd(ace_dtype dtype, ace_input_mode input_mode, int32_t 
                             const int32_t* expert_key, float alpha, const void* A, const void* B,
                             const ace_routing* adapter_rt, void* y, void* ws, size_t ws_bytes,
                             void* stream);
+
+/*
+ * Input gradient of the expert projection (the frozen experts' part of the
+ * backward of y[t*k + j, :] = W_e xin(t, j); the adapter's part is added by
+ * ace_grouped_lora_bwd / ace_expertwise_lora_bwd, which accumulate into dx):
+ *   ACE_INPUT_PER_PAIR: dx[t*k + j, :] = W_e^T dy[t*k + j, :]
+ *   ACE_INPUT_SHARED:   dx[t, :] = sum over the routed slots j of t of
+ *                       W_e^T dy[t*k + j, :],     e = topk_ids[t, j].
+ *   dy          device [T*k, d_out], dtype; rows of dropped pairs are not used.
+ *   W           device [E, d_out, d_in], dtype, as for ace_moe_lora_fwd.
+ *   expert_rt   rows from ace_group_permute in ACE_ROWS_EXPERT mode over E
+ *               experts.
+ *   accumulate  0: dx is written; 1: dx += (gate and up share their input).
+ *   dx          device, [T, d_in] (shared) or [T*k, d_in] (per pair), dtype.
+ *               Per pair, rows of dropped pairs are left untouched; shared, a
+ *               token without routed pairs gets 0 (accumulate: is left as it
+ *               was).  Must not overlap dy or W.
+ *   ws          device scratch of at least
+ *               ace_workspace_bytes(ACE_OP_MOE_DX, T, k, d_in, d_out, E, 0)
+ *               for the shared input or accumulate = 1, where it holds a row
+ *               of dtype per pair (the products are summed in fp32 and rounded
+ *               to dtype there; a token's rows are then added in fp32, in slot
+ *               order, and rounded once).  Not used, and may be NULL, for the
+ *               per-pair input with accumulate = 0.  No initialisation.
+ * Limits: T * k * d_out and T * k * d_in below 2^33 - 4096, d_in below 2^24.
+ * Deterministic.
+ */
+ace_status ace_moe_dx(ace_dtype dtype, ace_input_mode input_mode, int32_t T, int32_t k,
+                      int32_t d_in, int32_t d_out, int32_t E, const void* dy, const void* W,
+                      const ace_routing* expert_rt, int32_t accumulate, void* dx, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/*
+ * The layer output from the expert outputs (Sec. 3.1: every routed expert's
+ * output times its router weight), and its gradient:
+ *   out[t, :] = sum over the routed slots j of w[t, j] y[t*k + j, :]
+ *   dy[t*k + j, :] = w[t, j] dout[t, :],  dw[t, j] = <dout[t, :], y[t*k + j, :]>
+ *   y           device [T*k, d], dtype; rows of dropped pairs are not used.
+ *               Backward: may be NULL when dw is NULL.
+ *   pair_w      device fp32 [T, k] or NULL (weight 1).
+ *   rt          rows of the layer's routing, in any row mode (its pair_row
+ *               tells which pairs were dropped).
+ *   out         device [T, d], dtype: written (0 for a token without routed
+ *               pairs).  Summed in fp32 in slot order, rounded once.
+ *   dout        device [T, d], dtype.
+ *   dy          device [T*k, d], dtype: written; rows of dropped pairs are left
+ *               untouched.  May be y itself.
+ *   dw          device fp32 [T, k] or NULL: written (0 for dropped pairs).
+ * d must be a multiple of 8 (bf16) or 4 (f32); y, out, dout and dy 16-byte
+ * aligned.  T * k * d below 2^33 - 4096.  Deterministic.
+ */
+ace_status ace_moe_combine_fwd(ace_dtype dtype, int32_t T, int32_t k, int32_t d, const void* y,
+                               const float* pair_w, const ace_routing* rt, void* out,
+                               void* stream);
+ace_status ace_moe_combine_bwd(ace_dtype dtype, int32_t T, int32_t k, int32_t d, const void* dout,
+                               const void* y, const float* pair_w, const ace_routing* rt, void* dy,
+                               float* dw, void* stream);
+
+/*
+ * 8-bit checkpoints of activations: rows kept for the backward at 8.25 bits per
+ * element.  Blocks of 32 consecutive columns of a row (the last block of a row
+ * may be shorter) share one byte; code c and byte s stand for c * 2^(s - 133)
+ * (OCP MXINT8).  s is the exponent field of the block's largest |x| as an fp32
+ * number, plus one where that |x| would round to code 128 (never 255); codes are
+ * rounded to nearest even, at most 127 in size.  So a value is off by at most
+ * 2^(s - 134), that is the block's largest |x| / 127.5 (twice that where s
+ * would have to pass 254), and it is exact in bf16 as in fp32; zeros keep no
+ * sign.  A block that holds a NaN or an infinity gets s = 255 and codes 0, and
+ * reads back as NaN.
+ */
+typedef struct ace_packed_act {
+  int8_t* codes;  /* device [rows, d], 16-byte aligned                          */
+  uint8_t* exps;  /* device [rows, ceil(d / 32)]                                */
+} ace_packed_act;
+
+/*
+ *   rows, d     rows >= 0; d a multiple of 8 (bf16) or 4 (f32); rows * (d
+ *               rounded up to 32) below 2^33 - 4096.
+ *   x           device [rows, d], dtype, 16-byte aligned.
+ * ace_act_pack writes c from x, ace_act_unpack x from c.  No overlaps.
+ */
+ace_status ace_act_pack(ace_dtype dtype, int64_t rows, int32_t d, const void* x,
+                        const ace_packed_act* c, void* stream);
+ace_status ace_act_unpack(ace_dtype dtype, int64_t rows, int32_t d, const ace_packed_act* c,
+                          void* x, void* stream);
+
+/*
+ * SwiGLU between the gate/up and the down projections of an expert:
+ *   a  = g sigma(g) u,             sigma(g) = 1 / (1 + e^-g)
+ *   dg = da u sigma(g) (1 + g (1 - sigma(g))),   du = da g sigma(g)
+ * for every row (in fp32, each result rounded once; rows of dropped pairs give
+ * whatever their inputs make of them).
+ *   rows, d     as for ace_act_pack.
+ *   g, u, da    device [rows, d], dtype, 16-byte aligned.
+ *   a, dg, du   device [rows, d], dtype, 16-byte aligned: written.
+ *   g_packed, u_packed  both given or both NULL.  Where g and u are NULL, both
+ *               passes read these checkpoints in their place (the forward: to
+ *               form a, the down projection's input, once more for the
+ *               backward).  A forward that is given g and u writes their
+ *               checkpoints in the same pass; a backward takes one or the other.
+ * An output may be the same buffer as an input that has its type and shape
+ * (dg = g, du = u, a = g, ...); other overlaps are not allowed.
+ */
+ace_status ace_swiglu_fwd(ace_dtype dtype, int64_t rows, int32_t d, const void* g, const void* u,
+                          void* a, const ace_packed_act* g_packed, const ace_packed_act* u_packed,
+                          void* stream);
+ace_status ace_swiglu_bwd(ace_dtype dtype, int64_t rows, int32_t d, const void* da, const void* g,
+                          const void* u, const ace_packed_act* g_packed,
+                          const ace_packed_act* u_packed, void* dg, void* du, void* stream);
 
 /*
  * Pairwise linear CKA of the expert adapters of one layer on a shared probe

@@ -26,13 +26,14 @@ ACE_OK, ACE_ERR_INVALID_ARG, ACE_ERR_UNSUPPORTED, ACE_ERR_WORKSPACE, ACE_ERR_HIP
 ACE_F32, ACE_BF16 = 0, 1
 ACE_ROWS_GROUP_DEDUP, ACE_ROWS_GROUP_PAIRS, ACE_ROWS_EXPERT = 0, 1, 2
 ACE_INPUT_SHARED, ACE_INPUT_PER_PAIR, ACE_INPUT_COMBINED = 0, 1, 2
-ACE_OP_PERMUTE, ACE_OP_FWD, ACE_OP_BWD, ACE_OP_CKA = 0, 1, 2, 3
+ACE_OP_PERMUTE, ACE_OP_FWD, ACE_OP_BWD, ACE_OP_CKA, ACE_OP_MOE_DX = 0, 1, 2, 3, 4
 
 EXPORTS = ("ace_group_permute", "ace_group_expert_permute", "ace_grouped_lora_fwd", "ace_grouped_lora_bwd",
            "ace_expertwise_lora_fwd", "ace_expertwise_lora_bwd", "ace_workspace_bytes",
            "ace_routing_check", "ace_last_error", "ace_pairwise_cka", "ace_similarity_graph",
            "ace_louvain", "ace_group_anchors", "ace_consolidate_adapters", "ace_moe_lora_fwd",
-           "ace_group_permute_noalloc")
+           "ace_group_permute_noalloc", "ace_moe_dx", "ace_moe_combine_fwd", "ace_moe_combine_bwd",
+           "ace_act_pack", "ace_act_unpack", "ace_swiglu_fwd", "ace_swiglu_bwd")
 ACE_PERMUTE_SCRATCH_BYTES = 4 << 20
 
 
@@ -43,6 +44,10 @@ class AceRouting(ctypes.Structure):
                 ("row_pair", ctypes.c_void_p), ("pair_list", ctypes.c_void_p),
                 ("n_keys", ctypes.c_int32), ("mode", ctypes.c_int32),
                 ("T", ctypes.c_int32), ("k", ctypes.c_int32)]
+
+
+class AcePackedAct(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("exps", ctypes.c_void_p)]
 
 
 _i32, _f32, _vp, _sz = ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
@@ -88,6 +93,22 @@ _lib.ace_consolidate_adapters.restype = _i32
 _lib.ace_moe_lora_fwd.argtypes = [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _R, _i32, _vp,
                                   _vp, _f32, _vp, _vp, _R, _vp, _vp, _sz, _vp]
 _lib.ace_moe_lora_fwd.restype = _i32
+_i64, _K = ctypes.c_int64, ctypes.POINTER(AcePackedAct)
+_lib.ace_moe_dx.argtypes = [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _R, _i32, _vp, _vp,
+                            _sz, _vp]
+_lib.ace_moe_dx.restype = _i32
+_lib.ace_moe_combine_fwd.argtypes = [_i32, _i32, _i32, _i32, _vp, _vp, _R, _vp, _vp]
+_lib.ace_moe_combine_fwd.restype = _i32
+_lib.ace_moe_combine_bwd.argtypes = [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _R, _vp, _vp, _vp]
+_lib.ace_moe_combine_bwd.restype = _i32
+_lib.ace_act_pack.argtypes = [_i32, _i64, _i32, _vp, _K, _vp]
+_lib.ace_act_pack.restype = _i32
+_lib.ace_act_unpack.argtypes = [_i32, _i64, _i32, _K, _vp, _vp]
+_lib.ace_act_unpack.restype = _i32
+_lib.ace_swiglu_fwd.argtypes = [_i32, _i64, _i32, _vp, _vp, _vp, _K, _K, _vp]
+_lib.ace_swiglu_fwd.restype = _i32
+_lib.ace_swiglu_bwd.argtypes = [_i32, _i64, _i32, _vp, _vp, _vp, _K, _K, _vp, _vp, _vp]
+_lib.ace_swiglu_bwd.restype = _i32
 _lib.ace_last_error.argtypes = []
 _lib.ace_last_error.restype = ctypes.c_char_p
 
@@ -250,7 +271,8 @@ def ace_group_permute_noalloc(topk_ids: torch.Tensor, E: int,
     routing.check_capacity(T, k, n_keys)
     _check(_lib.ace_group_permute_noalloc(_ptr(topk_ids), T, k, E, _ptr(expert_to_group), G,
                                           mode, ctypes.byref(routing.c), _stream(stream)),
-           "ace_group_permute_noalloc")
+           "ace_group_permute_noalloc", "ace_moe_dx", "ace_moe_combine_fwd", "ace_moe_combine_bwd",
+           "ace_act_pack", "ace_act_unpack", "ace_swiglu_fwd", "ace_swiglu_bwd")
     return routing
 
 
@@ -475,3 +497,214 @@ def ace_moe_lora_fwd(x, W, expert_routing: Routing, y, key_rank: Optional[Sequen
                                  _ptr(y), _ptr(ws), 0 if ws is None else ws.numel(),
                                  _stream(stream)),
            "ace_moe_lora_fwd")
+
+
+def _on_device(t: torch.Tensor) -> torch.device:
+    """The device of a call's first tensor, which must be the current one: the
+    library launches on the current device's stream."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, which is not the current GPU")
+    return t.device
+
+
+def _alloc(make, stream, *shape, **kw):
+    """A tensor that belongs to the call's stream: filled there, and given out
+    again only behind the work queued there."""
+    if stream is None:
+        return make(*shape, **kw)
+    with torch.cuda.stream(stream):
+        return make(*shape, **kw)
+
+
+def _check_routing(routing: Routing, T: int, k: int, device) -> None:
+    if (routing.c.T, routing.c.k) != (T, k):
+        raise ValueError(f"routing was built for T={routing.c.T} k={routing.c.k}, the call has "
+                         f"T={T} k={k}")
+    if routing.pair_row.device != device:
+        raise ValueError(f"routing is on {routing.pair_row.device}, expected {device}")
+
+
+def ace_moe_dx(dy, W, expert_routing: Routing, dx=None, input_mode: int = ACE_INPUT_SHARED,
+               accumulate: bool = False, ws=None, stream=None) -> torch.Tensor:
+    """Input gradient of the frozen expert projection (include/ace.h): per pair
+    dx[t*k + j] = W_e^T dy[t*k + j], shared their sum over a token's slots.
+    dx None allocates it (per pair: zeros, so that dropped pairs give 0)."""
+    T, k = expert_routing.c.T, expert_routing.c.k
+    device = _on_device(W)
+    if W.dim() != 3:
+        raise ValueError(f"W must be [E, d_out, d_in], got {tuple(W.shape)}")
+    E, d_out, d_in = W.shape
+    dt = _dtype(W)
+    _check_routing(expert_routing, T, k, device)
+    _want("dy", dy, T * k * d_out, W.dtype, device)
+    shared = input_mode == ACE_INPUT_SHARED
+    rows = T if shared else T * k
+    if dx is None:
+        if accumulate:
+            raise ValueError("accumulate needs dx")
+        dx = _alloc(torch.empty if shared else torch.zeros, stream, rows, d_in, dtype=W.dtype,
+                    device=device)
+    _want("dx", dx, rows * d_in, W.dtype, device)
+    if ws is None and (shared or accumulate):
+        need = ace_workspace_bytes(ACE_OP_MOE_DX, T, k, d_in, d_out, E, 0)
+        ws = _alloc(torch.empty, stream, max(need, 256), dtype=torch.uint8, device=device)
+    _want("ws", ws, None, torch.uint8, device, optional=True)
+    _check(_lib.ace_moe_dx(dt, input_mode, T, k, d_in, d_out, E, _ptr(dy), _ptr(W),
+                           ctypes.byref(expert_routing.c), int(accumulate), _ptr(dx), _ptr(ws),
+                           0 if ws is None else ws.numel(), _stream(stream)),
+           "ace_moe_dx")
+    return dx
+
+
+def ace_moe_combine_fwd(y, routing: Routing, out=None, pair_w=None, stream=None) -> torch.Tensor:
+    """out[t] = sum over the routed slots j of pair_w[t, j] y[t*k + j]."""
+    T, k = routing.c.T, routing.c.k
+    device = _on_device(y)
+    if y.dim() != 2 or y.shape[0] != T * k:
+        raise ValueError(f"y must be [T*k={T * k}, d], got {tuple(y.shape)}")
+    d = y.shape[1]
+    dt = _dtype(y)
+    _check_routing(routing, T, k, device)
+    _want("pair_w", pair_w, T * k, torch.float32, device, optional=True)
+    if out is None:
+        out = _alloc(torch.empty, stream, T, d, dtype=y.dtype, device=device)
+    _want("out", out, T * d, y.dtype, device)
+    _check(_lib.ace_moe_combine_fwd(dt, T, k, d, _ptr(y), _ptr(pair_w), ctypes.byref(routing.c),
+                                    _ptr(out), _stream(stream)), "ace_moe_combine_fwd")
+    return out
+
+
+def ace_moe_combine_bwd(dout, routing: Routing, dy=None, pair_w=None, y=None, dw=None,
+                        stream=None) -> torch.Tensor:
+    """dy[t*k + j] = pair_w[t, j] dout[t]; with dw also dw[t, j] = <dout[t], y[t*k + j]>.
+    dy None allocates it (zeros, so that dropped pairs give 0)."""
+    T, k = routing.c.T, routing.c.k
+    device = _on_device(dout)
+    if dout.dim() != 2 or dout.shape[0] != T:
+        raise ValueError(f"dout must be [T={T}, d], got {tuple(dout.shape)}")
+    d = dout.shape[1]
+    dt = _dtype(dout)
+    _check_routing(routing, T, k, device)
+    _want("pair_w", pair_w, T * k, torch.float32, device, optional=True)
+    _want("y", y, T * k * d, dout.dtype, device, optional=dw is None)
+    _want("dw", dw, T * k, torch.float32, device, optional=True)
+    if dy is None:
+        dy = _alloc(torch.zeros, stream, T * k, d, dtype=dout.dtype, device=device)
+    _want("dy", dy, T * k * d, dout.dtype, device)
+    _check(_lib.ace_moe_combine_bwd(dt, T, k, d, _ptr(dout), _ptr(y), _ptr(pair_w),
+                                    ctypes.byref(routing.c), _ptr(dy), _ptr(dw), _stream(stream)),
+           "ace_moe_combine_bwd")
+    return dy
+
+
+class PackedAct:
+    """Owns the device arrays of an ace_packed_act: activation rows [rows, d]
+    at 8.25 bits per element."""
+
+    def __init__(self, rows: int, d: int, device="cuda"):
+        self.rows, self.d = int(rows), int(d)
+        self.codes = torch.empty(self.rows, self.d, dtype=torch.int8, device=device)
+        self.exps = torch.empty(self.rows, -(-self.d // 32), dtype=torch.uint8, device=device)
+        self.c = AcePackedAct(self.codes.data_ptr() or None, self.exps.data_ptr() or None)
+
+
+def _want_packed(name: str, c: PackedAct, rows: int, d: int, device) -> None:
+    if not isinstance(c, PackedAct):
+        raise TypeError(f"{name} must be a PackedAct")
+    if (c.rows, c.d) != (rows, d):
+        raise ValueError(f"{name} holds [{c.rows}, {c.d}], expected [{rows}, {d}]")
+    if c.codes.device != device:
+        raise ValueError(f"{name} is on {c.codes.device}, expected {device}")
+
+
+def ace_act_pack(x, packed: Optional[PackedAct] = None, stream=None) -> PackedAct:
+    """8-bit checkpoint of the rows x [rows, d] (include/ace.h)."""
+    device = _on_device(x)
+    if x.dim() != 2:
+        raise ValueError(f"x must be [rows, d], got {tuple(x.shape)}")
+    rows, d = x.shape
+    dt = _dtype(x)
+    if packed is None:
+        packed = _alloc(PackedAct, stream, rows, d, device=device)
+    _want_packed("packed", packed, rows, d, device)
+    _check(_lib.ace_act_pack(dt, rows, d, _ptr(x), ctypes.byref(packed.c), _stream(stream)),
+           "ace_act_pack")
+    return packed
+
+
+def ace_act_unpack(packed: PackedAct, x=None, dtype=None, stream=None) -> torch.Tensor:
+    """The rows that a checkpoint stands for: into x, or a new tensor of dtype
+    (bf16 by default; the values are exact in both types)."""
+    device = _on_device(packed.codes)
+    rows, d = packed.rows, packed.d
+    if x is None:
+        x = _alloc(torch.empty, stream, rows, d, dtype=dtype or torch.bfloat16, device=device)
+    _want("x", x, rows * d, dtype, device)
+    _check(_lib.ace_act_unpack(_dtype(x), rows, d, ctypes.byref(packed.c), _ptr(x),
+                               _stream(stream)), "ace_act_unpack")
+    return x
+
+
+def _gate_up(g, u, rows: int, d: int, dtype, device):
+    """(g, u, g_packed, u_packed) as the library takes them: pointers of the
+    tensors, or None and the checkpoints."""
+    packed = isinstance(g, PackedAct)
+    if packed != isinstance(u, PackedAct):
+        raise TypeError("g and u must both be tensors or both be PackedAct")
+    for name, t in (("g", g), ("u", u)):
+        if packed:
+            _want_packed(name, t, rows, d, device)
+        else:
+            _want(name, t, rows * d, dtype, device)
+    if packed:
+        return None, None, ctypes.byref(g.c), ctypes.byref(u.c)
+    return _ptr(g), _ptr(u), None, None
+
+
+def ace_swiglu_fwd(g, u, a=None, g_packed: Optional[PackedAct] = None,
+                   u_packed: Optional[PackedAct] = None, dtype=None, stream=None) -> torch.Tensor:
+    """a = g sigmoid(g) u per row.  g and u are tensors (with g_packed and
+    u_packed their 8-bit checkpoints are written in the same pass) or both
+    PackedAct (then a, or dtype, tells the type: bf16 by default)."""
+    packed = isinstance(g, PackedAct)
+    device = _on_device(g.codes if packed else g)
+    if not packed and g.dim() != 2:
+        raise ValueError(f"g must be [rows, d], got {tuple(g.shape)}")
+    rows, d = (g.rows, g.d) if packed else g.shape
+    if packed and (g_packed is not None or u_packed is not None):
+        raise ValueError("g and u are checkpoints already")
+    if dtype is None:
+        dtype = g.dtype if not packed else a.dtype if a is not None else torch.bfloat16
+    gp, up, g8, u8 = _gate_up(g, u, rows, d, dtype, device)
+    if a is None:
+        a = _alloc(torch.empty, stream, rows, d, dtype=dtype, device=device)
+    _want("a", a, rows * d, dtype, device)
+    for name, c in (("g_packed", g_packed), ("u_packed", u_packed)):
+        if c is not None:
+            _want_packed(name, c, rows, d, device)
+    if g_packed is not None:
+        g8 = ctypes.byref(g_packed.c)
+    if u_packed is not None:
+        u8 = ctypes.byref(u_packed.c)
+    _check(_lib.ace_swiglu_fwd(_dtype(a), rows, d, gp, up, _ptr(a), g8, u8, _stream(stream)),
+           "ace_swiglu_fwd")
+    return a
+
+
+def ace_swiglu_bwd(da, g, u, dg=None, du=None, stream=None):
+    """(dg, du) of ace_swiglu_fwd; g and u are the forward's tensors or, both,
+    their checkpoints (PackedAct)."""
+    device = _on_device(da)
+    if da.dim() != 2:
+        raise ValueError(f"da must be [rows, d], got {tuple(da.shape)}")
+    rows, d = da.shape
+    gp, up, g8, u8 = _gate_up(g, u, rows, d, da.dtype, device)
+    if dg is None:
+        dg = _alloc(torch.empty, stream, rows, d, dtype=da.dtype, device=device)
+    if du is None:
+        du = _alloc(torch.empty, stream, rows, d, dtype=da.dtype, device=device)
+    _want("dg", dg, rows * d, da.dtype, device)
+    _want("du", du, rows * d, da.dtype, device)
+    _check(_lib.ace_swiglu_bwd(_dtype(da), rows, d, _ptr(da), gp, up, g8, u8, _ptr(dg), _ptr(du),
+                               _stream(stream)), "ace_swiglu_bwd")
+    return dg, du

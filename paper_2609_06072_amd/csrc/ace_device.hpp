@@ -35,6 +35,21 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
+// Division of numbers below 2^31 by d, 1 <= d < 2^31 (one high product and a
+// shift): with 2^l >= d > 2^(l-1) and mul = ceil(2^(31 + l) / d) < 2^32, idx mul
+// / 2^(31 + l) passes idx / d by less than idx 2^l / (d 2^(31 + l)) < 1 / d.
+struct FastDiv {
+  uint32_t d, mul, shift;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t div) : d(div), mul(0), shift(0) {
+    int l = 1;
+    while ((1u << l) < div) ++l;
+    shift = l - 1;
+    mul = (uint32_t)((((uint64_t)1 << (31 + l)) + div - 1) / div);
+  }
+  __device__ inline uint32_t div(uint32_t idx) const { return d == 1 ? idx : __umulhi(idx, mul) >> shift; }
+};
+
 // Per-key ranks and rank offsets, passed by value in the kernel arguments so
 // that no host-to-device copy precedes a launch.
 struct KeyTable {

@@ -123,6 +123,49 @@ struct MoeArgs {
   uint8_t key_of[kMaxKeys];   // adapter key of each expert
 };
 hipError_t launch_moe_gemm(int dtype, const MoeArgs& a, long P, hipStream_t stream);
+// The input gradient of the expert projection, y[p] = W_e^T x[p] per pair: x is
+// the output's gradient [T*k][d_in], W [E][d_in][d_out] (d_in, d_out: the
+// product's own contraction length and columns), per_pair, no adapter.
+hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream);
+
+// Weighted sum of a token's expert outputs, and its gradient (combine.hip).
+struct CombineArgs {
+  const void* y;              // [T*k][d]
+  const int32_t* pair_row;    // [T*k], negative where the pair was dropped
+  const float* pair_w;        // [T*k] or null (weight 1)
+  void* out;                  // [T][d], written (accumulate: added to)
+  int32_t k, d, accumulate;
+  FastDiv per_row;            // pieces of a row (set by the launcher)
+  uint32_t pieces;
+};
+hipError_t launch_combine_fwd(int dtype, CombineArgs a, int T, hipStream_t stream);
+struct CombineBwdArgs {
+  const void* dout;           // [T][d]
+  const void* y;              // [T*k][d], read for dw only
+  const int32_t* pair_row;
+  const float* pair_w;
+  void* dy;                   // [T*k][d]
+  float* dw;                  // [T*k] or null
+  long P;
+  int32_t k, d;
+};
+hipError_t launch_combine_bwd(int dtype, const CombineBwdArgs& a, hipStream_t stream);
+
+// Activations and their 8-bit checkpoints (activation.hip).
+struct ActGeom {
+  FastDiv per_row;            // pieces of a row, filled up to whole blocks
+  uint32_t pieces;            // of all rows
+  int32_t d;
+};
+struct SwigluArgs {
+  const void *da, *g, *u;     // [rows][d]
+  ace_packed_act g8, u8;      // checkpoints (codes null: none)
+  void *a, *dg, *du;
+};
+hipError_t launch_act_pack(int dtype, long rows, int d, const void* x, const ace_packed_act& c, hipStream_t stream);
+hipError_t launch_act_unpack(int dtype, long rows, int d, const ace_packed_act& c, void* x, hipStream_t stream);
+hipError_t launch_swiglu_fwd(int dtype, long rows, int d, const SwigluArgs& w, hipStream_t stream);
+hipError_t launch_swiglu_bwd(int dtype, long rows, int d, const SwigluArgs& w, hipStream_t stream);
 
 // Backward helpers shared with the pre-combined mode.
 //   prep: A^T [d_in][R] into At and B_q^T rows [R][d_out] into Bt (each

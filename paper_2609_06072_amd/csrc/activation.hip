@@ -1,0 +1,253 @@
+// SwiGLU between the gate/up and the down projections, and 8-bit checkpoints
+// of activations for the backward.
+//
+//   a  = g sigma(g) u
+//   dg = da u sigma(g) (1 + g (1 - sigma(g))),   du = da g sigma(g)
+//
+// Checkpoint (the OCP MXINT8 value): 32 columns of a row share the byte s,
+//   s     = exponent field of the block's largest |x| as an fp32 number, plus one
+//           where that |x| would round to code 128 (s stays below 255),
+//   code  = x 2^(133 - s) rounded to nearest even, at most 127 in size,
+//   value = code 2^(s - 133).
+// Scaling by a power of two is exact, so the one rounding fixes every bit, and
+// a value's seven bits are exact in bf16.  An error is at most half a step,
+// 2^(s - 134) <= amax / 127.5 (one step where s would pass 254).  A block that
+// holds a NaN or an infinity gets s = 255 and reads back as NaN.
+//
+// Everything here is bound by HBM.  A thread takes one 16-byte piece (8 bf16 or
+// 4 fp32 columns) of a row at a time, so a block's four or eight pieces sit in
+// neighbouring lanes: its largest |x| comes from two or three lane exchanges,
+// without LDS.  Rows are filled up to whole blocks (lanes past the row's end
+// hold zeros and store nothing).
+#include "ace_device.hpp"
+#include "ace_internal.hpp"
+
+namespace ace {
+
+namespace {
+
+constexpr int kBlockCols = 32;
+
+template <typename T>
+struct Pieces {
+  static constexpr int PER = Tr<T>::PER, PPB = kBlockCols / PER;   // pieces per block
+};
+
+// The codes of one piece: PER bytes.
+template <typename T>
+struct CodeWord;
+template <>
+struct CodeWord<__bf16> {
+  using type = u32x2;
+  __device__ static inline uint32_t word(type c, int i) { return c[i]; }
+};
+template <>
+struct CodeWord<float> {
+  using type = uint32_t;
+  __device__ static inline uint32_t word(type c, int) { return c; }
+};
+
+// s of the block that this lane's PER values belong to (all lanes of the
+// block get it).
+template <typename T>
+__device__ inline uint32_t block_exp(const float* v) {
+  uint32_t top = 0;   // |x| as bits: ordered like the numbers, NaN above infinity
+#pragma unroll
+  for (int i = 0; i < Tr<T>::PER; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < Pieces<T>::PPB; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  const uint32_t s = top >> 23;
+  const float m = __uint_as_float(top) * __uint_as_float(s >= 254 ? 0x00400000u : (254u - s) << 23) * 64.f;
+  return s < 254 && m >= 127.5f ? s + 1 : s;
+}
+
+template <typename T>
+__device__ inline typename CodeWord<T>::type encode(const float* v, uint32_t s) {
+  // 2^(127 - s), the power of two below the smallest normal number for 254
+  const float inv = __uint_as_float(s >= 254 ? 0x00400000u : (254u - s) << 23);
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < Tr<T>::PER; ++i) {
+    const float c = fminf(fmaxf(rintf(v[i] * inv * 64.f), -127.f), 127.f);
+    w[i / 4] |= (s == 255 ? 0u : (uint32_t)(int)c & 255u) << (8 * (i & 3));
+  }
+  if constexpr (Tr<T>::PER == 8) return u32x2{w[0], w[1]};
+  else return w[0];
+}
+
+template <typename T>
+__device__ inline void decode(typename CodeWord<T>::type c, uint32_t s, float* v) {
+  // 2^(s - 127); in two factors, as 2^(s - 133) may lie below the smallest normal number
+  const float scale = __uint_as_float(s == 255 ? 0x7fc00000u : s == 0 ? 0x00400000u : s << 23);
+#pragma unroll
+  for (int i = 0; i < Tr<T>::PER; ++i)
+    v[i] = (float)(int8_t)(CodeWord<T>::word(c, i / 4) >> (8 * (i & 3))) * 0.015625f * scale;
+}
+
+// Where a thread's piece lies.  Pieces past the row's end belong to the
+// row's last block.
+struct Spot {
+  bool in;        // inside the row
+  size_t elem;    // first element of the piece
+  size_t block;   // index of its block's s
+  bool first;     // first piece of the block (stores s)
+};
+template <typename T>
+__device__ inline Spot spot(const ActGeom& a, uint32_t idx) {
+  constexpr int PER = Pieces<T>::PER, PPB = Pieces<T>::PPB;
+  const uint32_t row = a.per_row.div(idx), pc = idx - row * a.per_row.d;
+  return Spot{idx < a.pieces && pc * PER < (uint32_t)a.d, (size_t)row * a.d + pc * PER,
+              (size_t)row * (a.per_row.d / PPB) + pc / PPB, pc % PPB == 0};
+}
+
+template <typename T>
+__device__ inline void load_piece(const void* p, const Spot& s, float* v) {
+  typename Tr<T>::frag f = Tr<T>::zero();
+  if (s.in) f = Tr<T>::load(static_cast<const T*>(p) + s.elem);
+  Tr<T>::to_f32(f, v);
+}
+
+template <typename T>
+__device__ inline void store_packed(const ace_packed_act& c, const Spot& s, const float* v) {
+  const uint32_t e = block_exp<T>(v);
+  if (!s.in) return;
+  *reinterpret_cast<typename CodeWord<T>::type*>(c.codes + s.elem) = encode<T>(v, e);
+  if (s.first) c.exps[s.block] = (uint8_t)e;
+}
+
+template <typename T>
+__device__ inline void load_packed(const ace_packed_act& c, const Spot& s, float* v) {
+  decode<T>(*reinterpret_cast<const typename CodeWord<T>::type*>(c.codes + s.elem), c.exps[s.block], v);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void pack_kernel(ActGeom a, const void* x, ace_packed_act c) {
+  const Spot s = spot<T>(a, blockIdx.x * kThreads + threadIdx.x);
+  float v[Tr<T>::PER];
+  load_piece<T>(x, s, v);
+  store_packed<T>(c, s, v);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void unpack_kernel(ActGeom a, ace_packed_act c, void* x) {
+  const Spot s = spot<T>(a, blockIdx.x * kThreads + threadIdx.x);
+  if (!s.in) return;
+  float v[Tr<T>::PER];
+  load_packed<T>(c, s, v);
+  Tr<T>::store(static_cast<T*>(x) + s.elem, Tr<T>::from_f32(v));
+}
+
+// sigma(g) and 1 - sigma(g) without overflow or cancellation: with
+// t = exp(-|g|), one of them is 1 / (1 + t) and the other t / (1 + t).
+__device__ inline void sigmoid2(float g, float& sig, float& one_minus) {
+  const float t = expf(-fabsf(g)), p = 1.f / (1.f + t), q = t * p;
+  sig = g < 0.f ? q : p;
+  one_minus = g < 0.f ? p : q;
+}
+
+// Where g and u come from, and whether their checkpoints are written.
+enum { kPlain, kWritePacked, kReadPacked };
+
+template <typename T, int CKPT>
+__device__ inline void load_gu(const SwigluArgs& w, const Spot& s, float* g, float* u) {
+  if (CKPT == kReadPacked) {
+    load_packed<T>(w.g8, s, g);
+    load_packed<T>(w.u8, s, u);
+  } else {
+    load_piece<T>(w.g, s, g);
+    load_piece<T>(w.u, s, u);
+  }
+}
+
+template <typename T, int CKPT>
+__global__ __launch_bounds__(kThreads) void swiglu_fwd_kernel(ActGeom a, SwigluArgs w) {
+  constexpr int PER = Tr<T>::PER;
+  const Spot s = spot<T>(a, blockIdx.x * kThreads + threadIdx.x);
+  float g[PER], u[PER], o[PER];
+  load_gu<T, CKPT>(w, s, g, u);
+  if (CKPT == kWritePacked) {
+    store_packed<T>(w.g8, s, g);
+    store_packed<T>(w.u8, s, u);
+  }
+  if (!s.in) return;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    float sig, rest;
+    sigmoid2(g[i], sig, rest);
+    o[i] = g[i] * sig * u[i];
+  }
+  Tr<T>::store(static_cast<T*>(w.a) + s.elem, Tr<T>::from_f32(o));
+}
+
+template <typename T, int CKPT>
+__global__ __launch_bounds__(kThreads) void swiglu_bwd_kernel(ActGeom a, SwigluArgs w) {
+  constexpr int PER = Tr<T>::PER;
+  const Spot s = spot<T>(a, blockIdx.x * kThreads + threadIdx.x);
+  if (!s.in) return;
+  float da[PER], g[PER], u[PER], dg[PER], du[PER];
+  load_piece<T>(w.da, s, da);
+  load_gu<T, CKPT>(w, s, g, u);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    float sig, rest;
+    sigmoid2(g[i], sig, rest);
+    dg[i] = da[i] * u[i] * (sig * (1.f + g[i] * rest));
+    du[i] = da[i] * (g[i] * sig);
+  }
+  Tr<T>::store(static_cast<T*>(w.dg) + s.elem, Tr<T>::from_f32(dg));
+  Tr<T>::store(static_cast<T*>(w.du) + s.elem, Tr<T>::from_f32(du));
+}
+
+// Pieces of the rows, filled up to whole blocks.
+ActGeom geometry(int dtype, long rows, int d) {
+  const int per = dtype == ACE_BF16 ? 8 : 4;
+  const int row = (d + kBlockCols - 1) / kBlockCols * (kBlockCols / per);
+  return ActGeom{FastDiv(row), (uint32_t)(rows * row), d};
+}
+
+template <typename T>
+void swiglu_fwd(const ActGeom& a, const SwigluArgs& w, unsigned grid, hipStream_t stream) {
+  if (!w.g8.codes) swiglu_fwd_kernel<T, kPlain><<<grid, kThreads, 0, stream>>>(a, w);
+  else if (w.g) swiglu_fwd_kernel<T, kWritePacked><<<grid, kThreads, 0, stream>>>(a, w);
+  else swiglu_fwd_kernel<T, kReadPacked><<<grid, kThreads, 0, stream>>>(a, w);
+}
+
+template <typename T>
+void swiglu_bwd(const ActGeom& a, const SwigluArgs& w, unsigned grid, hipStream_t stream) {
+  if (w.g) swiglu_bwd_kernel<T, kPlain><<<grid, kThreads, 0, stream>>>(a, w);
+  else swiglu_bwd_kernel<T, kReadPacked><<<grid, kThreads, 0, stream>>>(a, w);
+}
+
+}  // namespace
+
+hipError_t launch_act_pack(int dtype, long rows, int d, const void* x, const ace_packed_act& c, hipStream_t stream) {
+  const ActGeom a = geometry(dtype, rows, d);
+  const unsigned grid = (a.pieces + kThreads - 1) / kThreads;
+  if (dtype == ACE_BF16) pack_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a, x, c);
+  else pack_kernel<float><<<grid, kThreads, 0, stream>>>(a, x, c);
+  return hipGetLastError();
+}
+
+hipError_t launch_act_unpack(int dtype, long rows, int d, const ace_packed_act& c, void* x, hipStream_t stream) {
+  const ActGeom a = geometry(dtype, rows, d);
+  const unsigned grid = (a.pieces + kThreads - 1) / kThreads;
+  if (dtype == ACE_BF16) unpack_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a, c, x);
+  else unpack_kernel<float><<<grid, kThreads, 0, stream>>>(a, c, x);
+  return hipGetLastError();
+}
+
+hipError_t launch_swiglu_fwd(int dtype, long rows, int d, const SwigluArgs& w, hipStream_t stream) {
+  const ActGeom a = geometry(dtype, rows, d);
+  const unsigned grid = (a.pieces + kThreads - 1) / kThreads;
+  dtype == ACE_BF16 ? swiglu_fwd<__bf16>(a, w, grid, stream) : swiglu_fwd<float>(a, w, grid, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_swiglu_bwd(int dtype, long rows, int d, const SwigluArgs& w, hipStream_t stream) {
+  const ActGeom a = geometry(dtype, rows, d);
+  const unsigned grid = (a.pieces + kThreads - 1) / kThreads;
+  dtype == ACE_BF16 ? swiglu_bwd<__bf16>(a, w, grid, stream) : swiglu_bwd<float>(a, w, grid, stream);
+  return hipGetLastError();
+}
+
+}  // namespace ace

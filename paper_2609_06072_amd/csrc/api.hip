@@ -1,6 +1,5 @@
 // C-ABI entry points of libace: argument validation on the host, then the
-// kernel launches of permute.hip, lora_fwd.hip and lora_bwd.hip on the
-// caller's stream.  No call allocates device memory or synchronises (except
+// kernel launches of the other sources on the caller's stream.  No call allocates device memory or synchronises (except
 // ace_routing_check).
 #include <stdarg.h>
 #include <stdio.h>
@@ -284,6 +283,170 @@ ace_status run_moe_fwd(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k,
   return hip_status(launch_moe_gemm(dtype, a, (long)T * k, st), "expert GEMM launch");
 }
 
+// Shared validation of the calls on whole rows: dtype and d.
+ace_status check_rows(ace_dtype dtype, int32_t d) {
+  if (dtype != ACE_F32 && dtype != ACE_BF16) return fail(ACE_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+  const int vec = dtype == ACE_BF16 ? 8 : 4;
+  if (d < 1) return fail(ACE_ERR_INVALID_ARG, "d = %d", d);
+  if (d % vec) return fail(ACE_ERR_UNSUPPORTED, "d (%d) must be a multiple of %d", d, vec);
+  return ACE_OK;
+}
+
+// Elements of a tensor of rows, so that its 16-byte pieces (four fp32) count
+// to below 2^31 with a block to spare.
+constexpr int64_t kMaxRowElems = ((int64_t)1 << 33) - 4096;
+
+size_t moe_dx_ws_bytes(int T, int k, int d_in) { return (size_t)T * k * d_in * sizeof(float); }
+
+ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, int32_t d_in,
+                      int32_t d_out, int32_t E, const void* dy, const void* W,
+                      const ace_routing* ert, int32_t accumulate, void* dx, void* ws,
+                      size_t ws_bytes, void* stream) {
+  if (dtype != ACE_F32 && dtype != ACE_BF16) return fail(ACE_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+  if (im != ACE_INPUT_SHARED && im != ACE_INPUT_PER_PAIR)
+    return fail(ACE_ERR_INVALID_ARG, "input mode must be ACE_INPUT_SHARED or ACE_INPUT_PER_PAIR");
+  if (T < 0) return fail(ACE_ERR_INVALID_ARG, "T = %d < 0", T);
+  if (k < 1 || k > kMaxK) return fail(ACE_ERR_UNSUPPORTED, "k = %d outside [1, %d]", k, kMaxK);
+  if ((int64_t)T * k >= (int64_t)1 << 31) return fail(ACE_ERR_UNSUPPORTED, "T*k >= 2^31");
+  const int vec = dtype == ACE_BF16 ? 8 : 4;
+  if (d_in < 1 || d_out < 1) return fail(ACE_ERR_INVALID_ARG, "d_in = %d, d_out = %d", d_in, d_out);
+  if (d_in % vec || d_out % vec)
+    return fail(ACE_ERR_UNSUPPORTED, "d_in (%d) and d_out (%d) must be multiples of %d", d_in,
+                d_out, vec);
+  if (E < 1 || E > kMaxKeys) return fail(ACE_ERR_UNSUPPORTED, "E = %d outside [1, %d]", E, kMaxKeys);
+  if ((int64_t)E * d_out * d_in >= (int64_t)1 << 40)
+    return fail(ACE_ERR_UNSUPPORTED, "expert weights too large");
+  if (d_in >= 1 << 24) return fail(ACE_ERR_UNSUPPORTED, "d_in = %d, at most 2^24 - 1", d_in);
+  if ((int64_t)T * k * d_out >= kMaxRowElems || (int64_t)T * k * d_in >= kMaxRowElems)
+    return fail(ACE_ERR_UNSUPPORTED, "T*k*d_out or T*k*d_in reaches 2^33 elements");
+  if (accumulate != 0 && accumulate != 1) return fail(ACE_ERR_INVALID_ARG, "accumulate = %d", accumulate);
+  if (!ert || !ert->offsets || (T > 0 && (!ert->row_token || !ert->row_slots || !ert->pair_row)))
+    return fail(ACE_ERR_INVALID_ARG, "expert routing is NULL");
+  if (ert->mode != ACE_ROWS_EXPERT || ert->n_keys != E)
+    return fail(ACE_ERR_INVALID_ARG, "expert_rt must be ACE_ROWS_EXPERT routing over %d experts", E);
+  if (ert->T != T || ert->k != k)
+    return fail(ACE_ERR_INVALID_ARG, "expert routing was built for T=%d k=%d, call has T=%d k=%d",
+                ert->T, ert->k, T, k);
+  if (T > 0 && (!dy || !W || !dx)) return fail(ACE_ERR_INVALID_ARG, "dy, W or dx is NULL");
+  if (!aligned(dy, 16) || !aligned(W, 16) || !aligned(dx, 16))
+    return fail(ACE_ERR_INVALID_ARG, "dy, W and dx must be 16-byte aligned");
+  const bool pair_rows = im == ACE_INPUT_SHARED || accumulate;
+  if (pair_rows) {
+    const size_t need = moe_dx_ws_bytes(T, k, d_in);
+    if (need > 0 && (!ws || ws_bytes < need))
+      return fail(ACE_ERR_WORKSPACE, "the input gradient needs %zu workspace bytes, got %zu", need,
+                  ws ? ws_bytes : (size_t)0);
+    if (!aligned(ws, 256)) return fail(ACE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  }
+  if (T == 0) return ok();
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  MoeArgs a{};
+  a.x = dy;
+  a.W = W;
+  a.offsets = ert->offsets;
+  a.row_token = ert->row_token;
+  a.row_slots = ert->row_slots;
+  a.E = E;
+  a.k = k;
+  a.d_in = d_out;    // the product contracts over the projection's outputs
+  a.d_out = d_in;
+  a.per_pair = 1;
+  a.y = pair_rows ? ws : dx;
+  hipError_t e = launch_moe_dx(dtype, a, (long)T * k, st);
+  if (e != hipSuccess || !pair_rows) return hip_status(e, "input gradient launch");
+  // the token's rows, or (per pair) each row as a token of its own
+  CombineArgs c{};
+  c.y = ws;
+  c.pair_row = ert->pair_row;
+  c.out = dx;
+  c.k = im == ACE_INPUT_SHARED ? k : 1;
+  c.d = d_in;
+  c.accumulate = accumulate;
+  return hip_status(launch_combine_fwd(dtype, c, im == ACE_INPUT_SHARED ? T : T * k, st),
+                    "input gradient sum launch");
+}
+
+// Validation of the combine calls up to their pointers.
+ace_status check_combine(ace_dtype dtype, int32_t T, int32_t k, int32_t d, const float* pair_w,
+                         const ace_routing* rt) {
+  ace_status s = check_rows(dtype, d);
+  if (s != ACE_OK) return s;
+  if (T < 0) return fail(ACE_ERR_INVALID_ARG, "T = %d < 0", T);
+  if (k < 1 || k > kMaxK) return fail(ACE_ERR_UNSUPPORTED, "k = %d outside [1, %d]", k, kMaxK);
+  if ((int64_t)T * k >= (int64_t)1 << 31) return fail(ACE_ERR_UNSUPPORTED, "T*k >= 2^31");
+  if ((int64_t)T * k * d >= kMaxRowElems) return fail(ACE_ERR_UNSUPPORTED, "T*k*d reaches 2^33 elements");
+  if (!rt || (T > 0 && !rt->pair_row)) return fail(ACE_ERR_INVALID_ARG, "routing is NULL");
+  if (rt->mode != ACE_ROWS_GROUP_DEDUP && rt->mode != ACE_ROWS_GROUP_PAIRS && rt->mode != ACE_ROWS_EXPERT)
+    return fail(ACE_ERR_INVALID_ARG, "routing has an unknown row mode %d", rt->mode);
+  if (rt->T != T || rt->k != k)
+    return fail(ACE_ERR_INVALID_ARG, "routing was built for T=%d k=%d, call has T=%d k=%d", rt->T,
+                rt->k, T, k);
+  if (!aligned(pair_w, 4)) return fail(ACE_ERR_INVALID_ARG, "pair_w misaligned");
+  return ACE_OK;
+}
+
+// Validation of the calls on activation rows: sizes.
+ace_status check_act(ace_dtype dtype, int64_t rows, int32_t d) {
+  ace_status s = check_rows(dtype, d);
+  if (s != ACE_OK) return s;
+  if (rows < 0) return fail(ACE_ERR_INVALID_ARG, "rows = %lld < 0", (long long)rows);
+  const int64_t row = ((int64_t)d + 31) / 32 * 32;
+  if (rows > 0 && (row >= (int64_t)1 << 28 || rows >= kMaxRowElems / row))
+    return fail(ACE_ERR_UNSUPPORTED, "%lld rows of %d columns reach 2^33 elements", (long long)rows, d);
+  return ACE_OK;
+}
+
+ace_status check_packed(const char* name, const ace_packed_act* c, int64_t rows) {
+  if (!c || (rows > 0 && (!c->codes || !c->exps))) return fail(ACE_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned(c->codes, 16)) return fail(ACE_ERR_INVALID_ARG, "%s's codes must be 16-byte aligned", name);
+  return ACE_OK;
+}
+
+ace_status check_act_tensor(const char* name, const void* p, int64_t rows) {
+  if (rows > 0 && !p) return fail(ACE_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned(p, 16)) return fail(ACE_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
+  return ACE_OK;
+}
+
+ace_status run_swiglu(bool bwd, ace_dtype dtype, int64_t rows, int32_t d, const void* da,
+                      const void* g, const void* u, const ace_packed_act* g8,
+                      const ace_packed_act* u8, void* dg, void* du, void* a, void* stream) {
+  ace_status s = check_act(dtype, rows, d);
+  if (s != ACE_OK) return s;
+  if ((g8 == nullptr) != (u8 == nullptr))
+    return fail(ACE_ERR_INVALID_ARG, "g_packed and u_packed must both be given or both be NULL");
+  const bool held = g8 && !g && !u;   // g and u come from their checkpoints
+  SwigluArgs w{};
+  if (g8) {
+    if ((s = check_packed("g_packed", g8, rows)) != ACE_OK) return s;
+    if ((s = check_packed("u_packed", u8, rows)) != ACE_OK) return s;
+    if (bwd && !held) return fail(ACE_ERR_INVALID_ARG, "both g, u and their checkpoints are given");
+    w.g8 = *g8;
+    w.u8 = *u8;
+  }
+  if (!held) {
+    if ((s = check_act_tensor("g", g, rows)) != ACE_OK) return s;
+    if ((s = check_act_tensor("u", u, rows)) != ACE_OK) return s;
+  }
+  if (bwd) {
+    if ((s = check_act_tensor("da", da, rows)) != ACE_OK) return s;
+    if ((s = check_act_tensor("dg", dg, rows)) != ACE_OK) return s;
+    if ((s = check_act_tensor("du", du, rows)) != ACE_OK) return s;
+  } else if ((s = check_act_tensor("a", a, rows)) != ACE_OK) {
+    return s;
+  }
+  if (rows == 0) return ok();
+  w.da = da;
+  w.g = g;
+  w.u = u;
+  w.a = a;
+  w.dg = dg;
+  w.du = du;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return bwd ? hip_status(launch_swiglu_bwd(dtype, rows, d, w, st), "swiglu backward launch")
+             : hip_status(launch_swiglu_fwd(dtype, rows, d, w, st), "swiglu forward launch");
+}
+
 }  // namespace
 
 int device_cu_count() {
@@ -430,6 +593,93 @@ ace_status ace_moe_lora_fwd(ace_dtype dtype, ace_input_mode input_mode, int32_t 
                             void* stream) {
   return run_moe_fwd(dtype, input_mode, T, k, d_in, d_out, E, x, W, expert_rt, n_keys, key_rank,
                      expert_key, alpha, A, B, adapter_rt, y, ws, ws_bytes, stream);
+}
+
+ace_status ace_moe_dx(ace_dtype dtype, ace_input_mode input_mode, int32_t T, int32_t k,
+                      int32_t d_in, int32_t d_out, int32_t E, const void* dy, const void* W,
+                      const ace_routing* expert_rt, int32_t accumulate, void* dx, void* ws,
+                      size_t ws_bytes, void* stream) {
+  return run_moe_dx(dtype, input_mode, T, k, d_in, d_out, E, dy, W, expert_rt, accumulate, dx, ws,
+                    ws_bytes, stream);
+}
+
+ace_status ace_moe_combine_fwd(ace_dtype dtype, int32_t T, int32_t k, int32_t d, const void* y,
+                               const float* pair_w, const ace_routing* rt, void* out,
+                               void* stream) {
+  ace_status s = check_combine(dtype, T, k, d, pair_w, rt);
+  if (s != ACE_OK) return s;
+  if (T > 0 && (!y || !out)) return fail(ACE_ERR_INVALID_ARG, "y or out is NULL");
+  if (!aligned(y, 16) || !aligned(out, 16))
+    return fail(ACE_ERR_INVALID_ARG, "y and out must be 16-byte aligned");
+  if (T == 0) return ok();
+  CombineArgs c{};
+  c.y = y;
+  c.pair_row = rt->pair_row;
+  c.pair_w = pair_w;
+  c.out = out;
+  c.k = k;
+  c.d = d;
+  return hip_status(launch_combine_fwd(dtype, c, T, static_cast<hipStream_t>(stream)), "combine launch");
+}
+
+ace_status ace_moe_combine_bwd(ace_dtype dtype, int32_t T, int32_t k, int32_t d, const void* dout,
+                               const void* y, const float* pair_w, const ace_routing* rt, void* dy,
+                               float* dw, void* stream) {
+  ace_status s = check_combine(dtype, T, k, d, pair_w, rt);
+  if (s != ACE_OK) return s;
+  if (T > 0 && (!dout || !dy)) return fail(ACE_ERR_INVALID_ARG, "dout or dy is NULL");
+  if (T > 0 && dw && !y) return fail(ACE_ERR_INVALID_ARG, "dw needs y");
+  if (!aligned(dout, 16) || !aligned(y, 16) || !aligned(dy, 16))
+    return fail(ACE_ERR_INVALID_ARG, "dout, y and dy must be 16-byte aligned");
+  if (!aligned(dw, 4)) return fail(ACE_ERR_INVALID_ARG, "dw misaligned");
+  if (T == 0) return ok();
+  CombineBwdArgs c{};
+  c.dout = dout;
+  c.y = y;
+  c.pair_row = rt->pair_row;
+  c.pair_w = pair_w;
+  c.dy = dy;
+  c.dw = dw;
+  c.P = (long)T * k;
+  c.k = k;
+  c.d = d;
+  return hip_status(launch_combine_bwd(dtype, c, static_cast<hipStream_t>(stream)),
+                    "combine backward launch");
+}
+
+ace_status ace_act_pack(ace_dtype dtype, int64_t rows, int32_t d, const void* x,
+                        const ace_packed_act* c, void* stream) {
+  ace_status s = check_act(dtype, rows, d);
+  if (s == ACE_OK) s = check_act_tensor("x", x, rows);
+  if (s == ACE_OK) s = check_packed("c", c, rows);
+  if (s != ACE_OK) return s;
+  if (rows == 0) return ok();
+  return hip_status(launch_act_pack(dtype, rows, d, x, *c, static_cast<hipStream_t>(stream)),
+                    "activation pack launch");
+}
+
+ace_status ace_act_unpack(ace_dtype dtype, int64_t rows, int32_t d, const ace_packed_act* c,
+                          void* x, void* stream) {
+  ace_status s = check_act(dtype, rows, d);
+  if (s == ACE_OK) s = check_act_tensor("x", x, rows);
+  if (s == ACE_OK) s = check_packed("c", c, rows);
+  if (s != ACE_OK) return s;
+  if (rows == 0) return ok();
+  return hip_status(launch_act_unpack(dtype, rows, d, *c, x, static_cast<hipStream_t>(stream)),
+                    "activation unpack launch");
+}
+
+ace_status ace_swiglu_fwd(ace_dtype dtype, int64_t rows, int32_t d, const void* g, const void* u,
+                          void* a, const ace_packed_act* g_packed, const ace_packed_act* u_packed,
+                          void* stream) {
+  return run_swiglu(false, dtype, rows, d, nullptr, g, u, g_packed, u_packed, nullptr, nullptr, a,
+                    stream);
+}
+
+ace_status ace_swiglu_bwd(ace_dtype dtype, int64_t rows, int32_t d, const void* da, const void* g,
+                          const void* u, const ace_packed_act* g_packed,
+                          const ace_packed_act* u_packed, void* dg, void* du, void* stream) {
+  return run_swiglu(true, dtype, rows, d, da, g, u, g_packed, u_packed, dg, du, nullptr, stream);
 }
 
 ace_status ace_grouped_lora_bwd(ace_dtype dtype, ace_input_mode input_mode, int32_t T,
@@ -630,6 +880,12 @@ size_t ace_workspace_bytes(ace_op op, int32_t T, int32_t k, int32_t d_in, int32_
         return (size_t)-1;
       }
       return round256(cka_ws_bytes(T, d_out, n_keys, r_max));
+    case ACE_OP_MOE_DX:
+      if (d_in < 1 || d_out < 1 || (int64_t)T * k >= (int64_t)1 << 31) {
+        fail(ACE_ERR_INVALID_ARG, "invalid workspace query");
+        return (size_t)-1;
+      }
+      return round256(moe_dx_ws_bytes(T, k, d_in));
   }
   fail(ACE_ERR_INVALID_ARG, "unknown op %d", (int)op);
   return (size_t)-1;

@@ -1,0 +1,542 @@
+"""GPU parity of the operators around the adapted expert projections against
+oracle/layer_oracle.py.
+
+Tolerances, per element, derived from the arithmetic (u = 2^-24 the half-step
+of fp32, h = 2^-8 that of bf16, u for fp32 outputs):
+  moe_dx    a product of K terms in fp32 matrix units, whose partial sums are
+            rounded or truncated once per term at most: K * 2^-23 * S with S the
+            sum of the terms' absolute values; a pair's row of the shared input
+            is rounded to dtype (h |c_j|, summed over the slots), the sum of k
+            rows adds k u S, and the result one rounding h |dx|.
+  combine   (k + 1) u sum |w y| and one rounding; dw: d products and sums of
+            fp32, at most (d / 64 + 7) * 2 roundings deep: (d/32 + 16) u S.
+  swiglu    t = e^-|g| within 2 ulp (4 u); 1 + t, the division, t p: at most
+            4 u + 3 u relative; three more products: 16 u covers a and du, and dg
+            on its terms' sizes (1 + |g| (1 - sigma)); one rounding.  Results
+            below the smallest normal number add 2^-126 at most for each factor.
+  checkpoint  bit for bit.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as L
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+H = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a HIP device")
+    from paper_2609_06072_amd import ace  # noqa: F401
+
+
+@pytest.fixture(scope="module")
+def ace():
+    from paper_2609_06072_amd import ace as mod
+    return mod
+
+
+def f64(t):
+    return t.detach().to("cpu", torch.float64).numpy()
+
+
+def gen(seed, *shape, dtype="bf16", scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(DT[dtype]).cuda()
+
+
+def close(name, got, ref, tol):
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    assert got.shape == ref.shape, name
+    bad = ~(np.abs(got - ref) <= tol)
+    assert not bad.any(), (f"{name}: {bad.sum()} of {bad.size} off, first at {np.argwhere(bad)[0]}: "
+                           f"{got[bad][0]} for {ref[bad][0]}, tolerance {np.broadcast_to(tol, ref.shape)[bad][0]}")
+
+
+def route(ace, ids, E):
+    return ace.ace_group_permute(torch.from_numpy(ids).cuda(), E, None, E, ace.ACE_ROWS_EXPERT)
+
+
+def draw_ids(T, k, E, seed, drop=0.0, skew=0.0):
+    rng = np.random.default_rng(seed)
+    logits = rng.gumbel(size=(T, E)) - skew * np.log(np.arange(1, E + 1))
+    ids = np.argsort(-logits, axis=1)[:, :k].astype(np.int32)
+    ids[rng.random((T, k)) < drop] = -1
+    return np.ascontiguousarray(ids)
+
+
+# ------------------------------------------------------------------ moe_dx
+
+def dx_refs(dy, W, ids, E, dtype, shared):
+    """(reference, tolerance)"""
+    k, K = ids.shape[1], W.shape[1]
+    c, S = L.expert_dx(dy, W, ids, E), L.expert_dx(dy, W, ids, E, absolute=True)
+    if not shared:
+        return c, H[dtype] * np.abs(c) * (1 + 2 ** -7) + K * 2.0 ** -23 * S + 1e-38
+    ref = L.slot_sum(c, k)
+    tol = (H[dtype] * (L.slot_sum(np.abs(c), k) + np.abs(ref)) * (1 + 2 ** -6)
+           + (K * 2.0 ** -23 + (k + 1) * U) * L.slot_sum(S, k) * (1 + 2 ** -6) + 1e-38)
+    return ref, tol
+
+
+DX_SIZES = [
+    # T, k, E, d_in, d_out, dropped, skew
+    (1, 1, 1, 8, 8, 0.0, 0.0),              # the smallest
+    (1, 4, 8, 264, 520, 0.0, 0.0),          # one token
+    (3, 2, 4, 40, 72, 0.0, 0.0),
+    (7, 8, 64, 128, 1032, 0.0, 0.8),        # most experts empty
+    (100, 2, 2, 248, 24, 0.0, 0.0),         # a contraction shorter than a stage
+    (130, 4, 7, 264, 136, 0.1, 0.8),
+    (200, 8, 16, 1000, 264, 0.0, 0.8),
+    (300, 2, 3, 520, 328, 0.05, 1.0),
+    (1030, 2, 4, 512, 256, 0.0, 0.0),       # several large tiles of an expert
+    (2100, 1, 2, 264, 136, 0.02, 0.0),
+    (257, 32, 40, 64, 48, 0.3, 0.0),        # the most slots
+    (90, 2, 256, 64, 64, 0.0, 0.0),         # the most experts
+]
+
+
+@pytest.mark.parametrize("size", DX_SIZES, ids=lambda s: "x".join(map(str, s[:5])))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_moe_dx(ace, size, dtype):
+    T, k, E, d_in, d_out, drop, skew = size
+    ids = draw_ids(T, k, E, 1, drop, skew)
+    rt = route(ace, ids, E)
+    dy = gen(2, T * k, d_out, dtype=dtype)
+    W = gen(3, E, d_out, d_in, dtype=dtype, scale=d_in ** -0.5)
+    dropped = ~L.routed(ids, E).reshape(-1)
+    dyn = dy.clone()
+    dyn[torch.from_numpy(dropped).cuda()] = float("nan")       # never used
+    hit = np.unique(ids[ids >= 0])
+    Wn = W.clone()
+    Wn[[e for e in range(E) if e not in hit]] = float("nan")   # experts without a pair
+    a, b = f64(dy), f64(W)
+    ref, tol = dx_refs(a, b, ids, E, dtype, False)
+    dx = torch.full((T * k, d_in), 7.0, dtype=DT[dtype], device="cuda")
+    out = ace.ace_moe_dx(dyn, Wn, rt, dx, input_mode=ace.ACE_INPUT_PER_PAIR)
+    assert out is dx
+    assert bool((dx[torch.from_numpy(dropped).cuda()] == 7.0).all())
+    close("per pair", f64(dx)[~dropped], ref[~dropped], tol[~dropped])
+    ref, tol = dx_refs(a, b, ids, E, dtype, True)
+    sh = ace.ace_moe_dx(dyn, Wn, rt)
+    close("shared", sh, ref, tol)
+    # added to what is there: one more rounding of the larger sum
+    base = gen(4, T, d_in, dtype=dtype)
+    acc = base.clone()
+    ace.ace_moe_dx(dyn, Wn, rt, acc, accumulate=True)
+    close("accumulated", acc, ref + f64(base), tol + H[dtype] * (np.abs(f64(base)) + np.abs(ref)) + 2 * U * np.abs(f64(base)))
+    base = gen(5, T * k, d_in, dtype=dtype)
+    acc = base.clone()
+    ace.ace_moe_dx(dyn, Wn, rt, acc, input_mode=ace.ACE_INPUT_PER_PAIR, accumulate=True)
+    ref, tol = dx_refs(a, b, ids, E, dtype, False)
+    close("accumulated per pair", acc, ref + f64(base), tol + H[dtype] * (np.abs(f64(base)) + np.abs(ref)) + 2 * U * np.abs(f64(base)))
+    assert torch.equal(acc[torch.from_numpy(dropped).cuda()], base[torch.from_numpy(dropped).cuda()])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_moe_dx_infinities_stay_in_their_rows(ace, dtype):
+    """An infinite gradient or weight reaches the results that use it and no
+    others: not the next pair's, and not through a ragged contraction."""
+    for rows in (3, 40, 300):
+        T, k, E, d_in, d_out = rows * 4, 1, 4, 72, 104
+        ids = (np.arange(T, dtype=np.int32) % E).reshape(T, 1)
+        rt = route(ace, ids, E)
+        dy = gen(6, T, d_out, dtype=dtype)
+        W = gen(7, E, d_out, d_in, dtype=dtype)
+        W[2, 0, :] = float("inf")        # expert 2 and dy's first column only
+        W[2, d_out - 1, :] = float("nan")
+        dy[5, :] = float("inf")
+        dx = ace.ace_moe_dx(dy, W, rt, input_mode=ace.ACE_INPUT_PER_PAIR)
+        clean = torch.from_numpy((ids[:, 0] != 2) & (np.arange(T) != 5)).cuda()
+        assert bool(torch.isfinite(dx[clean]).all())
+        assert not bool(torch.isfinite(dx[~clean]).any())
+        ref, tol = dx_refs(f64(torch.nan_to_num(dy, posinf=0)), f64(torch.nan_to_num(W, posinf=0)), ids, E, dtype, False)
+        keep = clean.cpu().numpy()
+        close("finite rows", f64(dx)[keep], ref[keep], tol[keep])
+
+
+def test_moe_dx_all_dropped_and_repeated(ace):
+    T, k, E, d = 5, 3, 4, 64
+    ids = np.full((T, k), -1, np.int32)
+    W, dy = gen(8, E, d, d), gen(9, T * k, d)
+    dx = ace.ace_moe_dx(dy, W, route(ace, ids, E))
+    assert dx.shape == (T, d) and not bool(dx.any())
+    ids[:] = 2                       # one pair of each token survives
+    dx = ace.ace_moe_dx(dy, W, route(ace, ids, E))
+    ref, tol = dx_refs(f64(dy), f64(W), ids, E, "bf16", True)
+    close("repeated ids", dx, ref, tol)
+
+
+@pytest.mark.parametrize("dtype,T,k,E,d_in,d_out", [
+    ("bf16", 5, 2, 8, 512, 520), ("bf16", 900, 2, 4, 520, 264), ("bf16", 400, 4, 32, 264, 520),
+    ("f32", 60, 2, 4, 136, 72), ("f32", 700, 2, 3, 264, 136)])
+def test_moe_dx_repeats_bit_for_bit(ace, dtype, T, k, E, d_in, d_out):
+    ids = draw_ids(T, k, E, 11)
+    rt = route(ace, ids, E)
+    dy, W = gen(12, T * k, d_out, dtype=dtype), gen(13, E, d_out, d_in, dtype=dtype)
+    a, b = ace.ace_moe_dx(dy, W, rt), ace.ace_moe_dx(dy, W, rt)
+    assert torch.equal(a, b)
+
+
+def test_moe_dx_agrees_with_the_forward(ace):
+    """<dy, W x> = <W^T dy, x>, with the library's own projection: both sides
+    are sums of T*k*d_out and T*d_in products whose factors are off by a
+    half-step of bf16 each."""
+    T, k, E, d_in, d_out = 200, 4, 8, 264, 520
+    ids = draw_ids(T, k, E, 14)
+    rt = route(ace, ids, E)
+    x, W, dy = gen(15, T, d_in), gen(16, E, d_out, d_in, scale=d_in ** -0.5), gen(17, T * k, d_out)
+    y = torch.empty(T * k, d_out, dtype=torch.bfloat16, device="cuda")
+    ace.ace_moe_lora_fwd(x, W, rt, y)
+    dx = ace.ace_moe_dx(dy, W, rt)
+    left, right = float((f64(dy) * f64(y)).sum()), float((f64(dx) * f64(x)).sum())
+    c = np.abs(L.expert_dx(f64(dy), f64(W), ids, E))
+    bound = H["bf16"] * (np.abs(f64(dy) * f64(y)).sum() + 2 * (L.slot_sum(c, k) * np.abs(f64(x))).sum())
+    assert abs(left - right) <= 1.1 * bound
+
+
+# ----------------------------------------------------------------- combine
+
+@pytest.mark.parametrize("T,k,d,drop", [(1, 1, 8, 0.0), (1, 8, 2048, 0.0), (3, 2, 40, 0.3), (130, 4, 1032, 0.1),
+                                        (77, 32, 136, 0.2), (1000, 6, 520, 0.0)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("weighted", [True, False])
+def test_combine(ace, T, k, d, drop, dtype, weighted):
+    E = 40
+    ids = draw_ids(T, k, E, 20, drop)
+    rt = route(ace, ids, E)
+    ok = L.routed(ids, E)
+    lost = torch.from_numpy(~ok.reshape(-1)).cuda()
+    y, dout = gen(21, T * k, d, dtype=dtype), gen(22, T, d, dtype=dtype)
+    g = torch.Generator().manual_seed(23)
+    w = torch.rand(T, k, generator=g).cuda()
+    wn = f64(w) if weighted else np.ones((T, k))
+    y[lost] = float("nan")
+    yc = f64(torch.nan_to_num(y))
+    arg = dict(pair_w=w if weighted else None)
+    out = ace.ace_moe_combine_fwd(y, rt, **arg)
+    ref = L.combine(yc, wn, ids, E)
+    S = L.combine(np.abs(yc), wn, ids, E)
+    close("out", out, ref, H[dtype] * np.abs(ref) * (1 + 2 ** -7) + (k + 1) * U * S + 1e-38)
+    dy = torch.full((T * k, d), 3.0, dtype=DT[dtype], device="cuda")
+    dw = torch.full((T, k), 9.0, device="cuda")
+    ace.ace_moe_combine_bwd(dout, rt, dy, y=y, dw=dw, **arg)
+    rdy, rdw = L.combine_grads(f64(dout), yc, wn, ids, E)
+    keep = ok.reshape(-1)
+    close("dy", f64(dy)[keep], rdy[keep], H[dtype] * np.abs(rdy[keep]) * (1 + 2 ** -7) + U * np.abs(rdy[keep]) + 1e-38)
+    assert bool((dy[lost] == 3.0).all())
+    _, S = L.combine_grads(np.abs(f64(dout)), np.abs(yc), wn, ids, E)
+    close("dw", dw, rdw, (d / 32 + 16) * U * S + 1e-38)
+    assert not bool(dw.view(-1)[lost].any())
+    # dy alone, and over y itself
+    dy2 = ace.ace_moe_combine_bwd(dout, rt, **arg)
+    assert torch.equal(dy2[~lost], dy[~lost]) and not bool(dy2[lost].any())
+    dw2 = torch.empty_like(dw)
+    ace.ace_moe_combine_bwd(dout, rt, y, y=y, dw=dw2, **arg)
+    assert torch.equal(y[~lost], dy[~lost]) and torch.equal(dw, dw2)
+
+
+def test_combine_any_row_mode(ace):
+    """Group-keyed routings tell the dropped pairs as well."""
+    T, k, E, d = 50, 4, 8, 64
+    ids = draw_ids(T, k, E, 24, 0.2)
+    e2g = torch.arange(E, dtype=torch.int32, device="cuda") // 2
+    y = gen(25, T * k, d)
+    want = ace.ace_moe_combine_fwd(y, route(ace, ids, E))
+    for mode in (ace.ACE_ROWS_GROUP_DEDUP, ace.ACE_ROWS_GROUP_PAIRS):
+        rt = ace.ace_group_permute(torch.from_numpy(ids).cuda(), E, e2g, 4, mode)
+        assert torch.equal(ace.ace_moe_combine_fwd(y, rt), want)
+
+
+# -------------------------------------------------------- checkpoint, swiglu
+
+def wide_values(n, d, dtype, seed):
+    """Values over the type's whole range, with zeros, ties, infinities, NaN."""
+    g = torch.Generator().manual_seed(seed)
+    e = torch.randint(-140, 120, (n, 1), generator=g) + torch.randint(0, 9, (n, d), generator=g)
+    x = torch.ldexp(torch.randn(n, d, generator=g, dtype=torch.float64), e).float()
+    steps = torch.randint(-255, 256, (n, d), generator=g) * 0.5          # half steps of 2^k
+    x = torch.where(torch.arange(n)[:, None] % 3 == 1, steps.float(), x)
+    x[torch.rand(n, d, generator=g) < 0.05] = 0.0
+    if n > 6:
+        x[2, d // 2], x[3, 0], x[4, d - 1] = float("nan"), float("inf"), float("-inf")
+        x[5] = 0.0
+        x[6, 0] = torch.finfo(torch.float32).max if dtype == "f32" else torch.finfo(torch.bfloat16).max
+    return x.to(DT[dtype])
+
+
+ACT_SIZES = [(1, 8), (1, 2048), (2, 40), (33, 24), (100, 1032), (7, 14336), (3000, 264), (513, 416)]
+
+
+@pytest.mark.parametrize("n,d", ACT_SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_checkpoint_bits(ace, n, d, dtype):
+    if dtype == "f32":
+        d += 4                                  # rows that are no multiple of 8
+    x = wide_values(n, d, dtype, 30)
+    codes, exps = L.pack(f64(x))
+    c = ace.ace_act_pack(x.cuda())
+    assert np.array_equal(c.exps.cpu().numpy(), exps)
+    assert np.array_equal(c.codes.cpu().numpy(), codes)
+    want = L.unpack(codes, exps)
+    for t in ("bf16", "f32") if d % 8 == 0 else ("f32",):
+        got = f64(ace.ace_act_unpack(c, dtype=DT[t]))
+        assert np.array_equal(got, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("rows", [0, 1, 5])
+def test_checkpoint_writes_its_rows_only(ace, rows):
+    n, d = 8, 40
+    c = ace.PackedAct(n, d)
+    c.codes.fill_(55)
+    c.exps.fill_(66)
+    part = ace.PackedAct(rows, d)
+    part.codes, part.exps = c.codes[:rows], c.exps[:rows]
+    part.c = ace.AcePackedAct(c.codes.data_ptr(), c.exps.data_ptr())
+    ace.ace_act_pack(gen(31, rows, d), part)
+    assert bool((c.codes[rows:] == 55).all()) and bool((c.exps[rows:] == 66).all())
+    x = torch.full((n, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    ace.ace_act_unpack(part, x[:rows])
+    assert bool((x[rows:] == 7.0).all())
+
+
+def swiglu_refs(da, g, u, dtype):
+    """name -> (reference, tolerance)"""
+    s = L.sigmoid(g)
+    dg, du = L.swiglu_grads(da, g, u)
+    a = L.swiglu(g, u)
+    h, tiny = H[dtype], 2.0 ** -126 * 4
+    size = np.abs(da * u) * s * (1 + np.abs(g) * (1 - s))
+    return {"a": (a, h * np.abs(a) + 17 * U * np.abs(a) + tiny * (1 + np.abs(g * u))),
+            "du": (du, h * np.abs(du) + 17 * U * np.abs(du) + tiny * (1 + np.abs(g * da))),
+            "dg": (dg, h * np.abs(dg) + 17 * U * size + tiny * (1 + np.abs(g * u * da)))}
+
+
+@pytest.mark.parametrize("n,d", ACT_SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_swiglu(ace, n, d, dtype):
+    g, u, da = (gen(s, n, d, dtype=dtype, scale=v) for s, v in ((40, 4.0), (41, 1.0), (42, 1.0)))
+    g[0, :8] = torch.tensor([0.0, -0.0, 80.0, -80.0, 120.0, -120.0, 1000.0, -1000.0], device="cuda").to(DT[dtype])
+    ref = swiglu_refs(f64(da), f64(g), f64(u), dtype)
+    a = ace.ace_swiglu_fwd(g, u)
+    close("a", a, *ref["a"])
+    dg, du = ace.ace_swiglu_bwd(da, g, u)
+    close("dg", dg, *ref["dg"])
+    close("du", du, *ref["du"])
+    # with checkpoints: the same a, the checkpoints of ace_act_pack, and
+    # gradients of what these hold
+    g8, u8 = ace.PackedAct(n, d), ace.PackedAct(n, d)
+    assert torch.equal(ace.ace_swiglu_fwd(g, u, g_packed=g8, u_packed=u8), a)
+    for x, c in ((g, g8), (u, u8)):
+        want = ace.ace_act_pack(x)
+        assert torch.equal(want.codes, c.codes) and torch.equal(want.exps, c.exps)
+    again = ace.ace_swiglu_fwd(g8, u8, dtype=DT[dtype])
+    dg8, du8 = ace.ace_swiglu_bwd(da, g8, u8)
+    held = [L.unpack(*L.pack(f64(x))) for x in (g, u)]
+    ref = swiglu_refs(f64(da), *held, dtype)
+    close("dg of the checkpoint", dg8, *ref["dg"])
+    close("du of the checkpoint", du8, *ref["du"])
+    close("a of the checkpoint", again, *ref["a"])
+    # outputs over the inputs
+    gi, ui, dai = g.clone(), u.clone(), da.clone()
+    ace.ace_swiglu_bwd(da, gi, ui, gi, ui)
+    assert torch.equal(gi, dg) and torch.equal(ui, du)
+    ace.ace_swiglu_bwd(dai, g8, u8, dai, ui)
+    assert torch.equal(dai, dg8) and torch.equal(ui, du8)
+    gi = g.clone()
+    ace.ace_swiglu_fwd(gi, u, gi)
+    assert torch.equal(gi, a)
+
+
+def test_swiglu_special_values(ace):
+    """NaN stays in its element; the block of a checkpoint loses all 32."""
+    g, u, da = gen(43, 4, 64), gen(44, 4, 64), gen(45, 4, 64)
+    g[1, 40], u[2, 3], g[3, 0] = float("nan"), float("inf"), float("inf")
+    g8, u8 = ace.PackedAct(4, 64), ace.PackedAct(4, 64)
+    a = ace.ace_swiglu_fwd(g, u, g_packed=g8, u_packed=u8)
+    bad = torch.zeros(4, 64, dtype=torch.bool, device="cuda")
+    bad[1, 40] = bad[2, 3] = bad[3, 0] = True
+    assert torch.equal(~torch.isfinite(a), bad)
+    dg, du = ace.ace_swiglu_bwd(da, g8, u8)
+    bad[1, 32:] = bad[2, :32] = bad[3, :32] = True
+    assert torch.equal(~torch.isfinite(dg), bad)
+
+
+# ------------------------------------------------------------ using them
+
+def test_refusals_leave_no_error_behind(ace):
+    x, rt = gen(50, 4, 64), route(ace, draw_ids(2, 2, 4, 51), 4)
+    W = gen(52, 4, 64, 64)
+    with pytest.raises(ValueError):
+        ace.ace_moe_dx(x[:, ::2], W, rt)                     # wrong size
+    with pytest.raises(ValueError):
+        ace.ace_moe_dx(x.t().contiguous().t(), W, rt)        # not contiguous
+    with pytest.raises(TypeError):
+        ace.ace_moe_dx(x.float(), W, rt)
+    with pytest.raises(TypeError):
+        ace.ace_act_pack(x.half())
+    with pytest.raises(ValueError):
+        ace.ace_moe_dx(x, W, rt, accumulate=True)            # nothing to add to
+    with pytest.raises(ace.AceError):
+        ace.ace_moe_dx(x, W, rt, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        ace.ace_act_pack(x, ace.PackedAct(4, 32))
+    with pytest.raises(TypeError):
+        ace.ace_swiglu_bwd(x, ace.PackedAct(4, 64), x)
+    with pytest.raises(ValueError):
+        ace.ace_moe_combine_bwd(x[:2], rt, dw=torch.empty(2, 2, device="cuda"))   # dw without y
+    ace.ace_moe_dx(x, W, rt)
+    torch.cuda.synchronize()
+
+
+def test_other_stream(ace):
+    """A call on a stream that is not the current one, with everything
+    allocated by the call."""
+    T, k, E, d = 300, 4, 8, 256
+    rt = route(ace, draw_ids(T, k, E, 53), E)
+    dy, W = gen(54, T * k, d), gen(55, E, d, d)
+    want = ace.ace_moe_dx(dy, W, rt), ace.ace_act_pack(dy), ace.ace_moe_combine_fwd(dy, rt)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = ace.ace_moe_dx(dy, W, rt, stream=s), ace.ace_act_pack(dy, stream=s), ace.ace_moe_combine_fwd(dy, rt, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+    assert torch.equal(got[1].codes, want[1].codes)
+
+
+class Layer:
+    """An adapted MoE layer with 8-bit checkpoints, forward and backward by the
+    library's calls: grouped gate and up, SwiGLU, expert-wise down, the weighted
+    sum."""
+
+    def __init__(self, T=150, d=264, f=136, E=8, k=2, r=4, seed=60):
+        rng = np.random.default_rng(seed)
+        self.T, self.d, self.f, self.E, self.k, self.r = T, d, f, E, k, r
+        self.e2g = np.repeat(np.arange(E // 2), 2).astype(np.int32)
+        self.G, self.ranks = E // 2, [2 * r] * (E // 2)
+        self.ids = draw_ids(T, k, E, seed, 0.05)
+        bf = lambda a: torch.from_numpy(a.astype(np.float32)).bfloat16().cuda()  # noqa: E731
+        self.ids_d, self.e2g_d = torch.from_numpy(self.ids).cuda(), torch.from_numpy(self.e2g).cuda()
+        self.w = torch.from_numpy(rng.random((T, k)).astype(np.float32)).cuda()
+        self.x, self.dout = bf(rng.normal(size=(T, d))), bf(rng.normal(size=(T, d)))
+        R = E * r
+        self.W = {n: bf(rng.normal(size=(E, o, i)) * i ** -0.5) for n, i, o in (("gate", d, f), ("up", d, f), ("down", f, d))}
+        self.A = {n: bf(rng.normal(size=(R, i)) * i ** -0.5) for n, i in (("gate", d), ("up", d), ("down", f))}
+        self.B = {n: bf(rng.normal(size=R * o) * 0.1) for n, o in (("gate", f), ("up", f), ("down", d))}
+        self.alpha = 16.0
+
+    def run(self, ace):
+        T, k, E, G = self.T, self.k, self.E, self.G
+        P, dev = T * k, "cuda"
+        bf = dict(dtype=torch.bfloat16, device=dev)
+        grt, ert = ace.ace_group_expert_permute(self.ids_d, E, self.e2g_d, G)
+        key, ew = [int(g) for g in self.e2g], ([self.r] * E, list(range(E)))
+        # forward; kept for the backward: x, and g and u in 8 bits
+        gate, up, y = (torch.zeros(P, n, **bf) for n in (self.f, self.f, self.d))
+        for n, t in (("gate", gate), ("up", up)):
+            ace.ace_moe_lora_fwd(self.x, self.W[n], ert, t, self.ranks, key, self.alpha, self.A[n], self.B[n], grt)
+        g8, u8 = ace.PackedAct(P, self.f), ace.PackedAct(P, self.f)
+        act = ace.ace_swiglu_fwd(gate, up, g_packed=g8, u_packed=u8)
+        x8 = ace.ace_act_pack(self.x)
+        ace.ace_moe_lora_fwd(act, self.W["down"], ert, y, *ew, self.alpha, self.A["down"], self.B["down"], ert,
+                             input_mode=ace.ACE_INPUT_PER_PAIR)
+        res = {"out": ace.ace_moe_combine_fwd(y, ert, pair_w=self.w)}
+        # backward
+        dw = torch.empty(T, k, device=dev)
+        dy = ace.ace_moe_combine_bwd(self.dout, ert, pair_w=self.w, y=y, dw=dw)
+        da = ace.ace_moe_dx(dy, self.W["down"], ert, input_mode=ace.ACE_INPUT_PER_PAIR)
+        act8 = ace.ace_swiglu_fwd(g8, u8)
+        dA, dB = ({n: torch.empty(t.shape, device=dev) for n, t in s.items()} for s in (self.A, self.B))
+        ace.ace_expertwise_lora_bwd(act8, self.A["down"], self.B["down"], E, self.r, self.alpha, ert, dy, da,
+                                    dA["down"], dB["down"], input_mode=ace.ACE_INPUT_PER_PAIR)
+        dg, du = ace.ace_swiglu_bwd(da, g8, u8)
+        xh = ace.ace_act_unpack(x8)
+        dx = ace.ace_moe_dx(dg, self.W["gate"], ert)
+        ace.ace_moe_dx(du, self.W["up"], ert, dx, accumulate=True)
+        for n, t in (("gate", dg), ("up", du)):
+            ace.ace_grouped_lora_bwd(xh, self.A[n], self.B[n], self.ranks, self.alpha, grt, t, dx, dA[n], dB[n])
+        res.update(dx=dx, dw=dw)
+        res.update({f"dA.{n}": t for n, t in dA.items()})
+        res.update({f"dB.{n}": t for n, t in dB.items()})
+        return res
+
+    def reference(self):
+        """The same layer through torch's differentiation in 64 bits on the CPU,
+        without roundings and checkpoints."""
+        E, k, r = self.E, self.k, self.r
+        d64 = lambda t: t.detach().cpu().double()  # noqa: E731
+        ok = torch.from_numpy(L.routed(self.ids, E))
+        x = d64(self.x).requires_grad_()
+        w = d64(self.w).requires_grad_()
+        A = {n: d64(t).requires_grad_() for n, t in self.A.items()}
+        B = {n: d64(t).requires_grad_() for n, t in self.B.items()}
+        W = {n: d64(t) for n, t in self.W.items()}
+
+        def proj(n, v, e, grouped):
+            o, q, rank = W[n].shape[1], int(self.e2g[e]) if grouped else e, 2 * r if grouped else r
+            lo = q * rank
+            b = B[n][o * lo:o * (lo + rank)].view(o, rank)
+            return W[n][e] @ v + self.alpha / rank * (b @ (A[n][lo:lo + rank] @ v))
+
+        rows = []
+        for t in range(self.T):
+            acc = torch.zeros(self.d, dtype=torch.float64)
+            for j in range(k):
+                if ok[t, j]:
+                    e = int(self.ids[t, j])
+                    g = proj("gate", x[t], e, True)
+                    u = proj("up", x[t], e, True)
+                    acc = acc + w[t, j] * proj("down", g * torch.sigmoid(g) * u, e, False)
+            rows.append(acc)
+        out = torch.stack(rows)
+        (out * d64(self.dout)).sum().backward()
+        res = {"out": out.detach(), "dx": x.grad, "dw": w.grad}
+        res.update({f"dA.{n}": t.grad for n, t in A.items()})
+        res.update({f"dB.{n}": t.grad for n, t in B.items()})
+        return {n: t.numpy() for n, t in res.items()}
+
+
+def test_layer_step(ace):
+    """Roundings of bf16 enter at about ten places in a row (rel. 2^-8 / sqrt(3)
+    each), and those of the checkpoints (at most amax/127.5 of a block, about
+    0.7% of a typical value) at one to three: below 2e-2 in the rel. L2 norm."""
+    lay = Layer()
+    got, ref = lay.run(ace), lay.reference()
+    assert got.keys() == ref.keys()
+    for n, r in ref.items():
+        err = np.linalg.norm(f64(got[n]) - r) / np.linalg.norm(r)
+        print(n, f"{err:.2e}", flush=True)
+        assert err <= 2e-2, n
+
+
+def test_layer_step_captured(ace):
+    """The step in a graph, replayed with other inputs in between and the same
+    ones again, beside eager runs."""
+    lay = Layer(T=90, seed=61)
+    first = {n: t.clone() for n, t in lay.run(ace).items()}
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        lay.run(ace)
+    torch.cuda.current_stream().wait_stream(s)
+    x0 = lay.x.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = lay.run(ace)
+    for replay in range(4):
+        lay.x.copy_(x0 if replay % 2 == 0 else -x0)
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = {n: t.clone() for n, t in got.items()}
+        eager = lay.run(ace)
+        for n, t in eager.items():
+            assert torch.equal(kept[n], t), (replay, n)
+            if replay % 2 == 0:
+                assert torch.equal(first[n], t), (replay, n)
