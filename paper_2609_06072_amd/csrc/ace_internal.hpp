@@ -112,6 +112,7 @@ struct MoeArgs {
   const int32_t* offsets;     // expert routing (ACE_ROWS_EXPERT)
   const int32_t* row_token;
   const uint32_t* row_slots;
+  const int32_t* pair_list;   // launch_moe_dx: pair of each row
   int32_t E, k, d_in, d_out, per_pair;
   const void* H;              // [U'][rpad] scaled shrink per adapter row, or null (no adapter)
   int32_t rpad;

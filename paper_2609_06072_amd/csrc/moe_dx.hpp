@@ -1,0 +1,325 @@
+// Input gradient of the expert projection, many rows per expert (part of
+// moe_gemm.hip): y[p] = W_e^T x[p] per pair, W_e [K][N] row-major, so the
+// contraction runs over W_e's rows.
+//
+// bf16, tiles of 256 rows x 256 columns, four waves of 128 x 128 as in
+// moe_gemm_large_kernel, with its ring of five 32 KB slots and its half-steps.
+// Two things differ:
+//   - A W unit is 64 contraction rows x 64 columns for each wx, and W fragments
+//     are transposed reads (two of 8 bytes in the place of one of 16).
+//   - A block stays and takes tile after tile, and the ring runs through:
+//     the last half-steps of a tile copy and read the first units of the next
+//     one, and a tile's results go from the accumulators to memory while these
+//     land.  (One block per tile spent about 14 us per tile outside its loop of
+//     14 to 28 us, with the matrix units and HBM busy in turns.)
+// A block's tiles are every 32nd of its XCD's run, so the blocks of an XCD work
+// on neighbouring tiles at a time.
+
+// Chunk swizzle of a 128-byte W^T row: pairs of chunks trade places, so that the
+// 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread
+// over the banks for the lanes of one g and of two.
+__device__ inline int lt_swz(int r) { return 2 * ((r & 3) ^ ((r >> 3) & 1)); }
+
+// Four values rounded to bf16, as two words.
+__device__ inline u32x2 round4(f32x4 v) {
+  return __builtin_bit_cast(u32x2, bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]});
+}
+
+// RAGGED: K is no multiple of two stages; the chunks past it are zeroed in the
+// fragments (see moe_gemm_large_kernel).  K >= kDxLargeK, so that the copies
+// never run ahead by more than a tile.
+constexpr int kDxLargeK = 256;
+
+template <bool RAGGED>
+__global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs a) {
+  using C = Large;
+  using F = bf16x8;
+  constexpr int ROWB = C::ROWB, NC = C::COPIES, KPL = kMaxKeys / 64;
+  __shared__ __attribute__((aligned(16))) char smem[C::SLOTS * C::SLOT];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, g = lane >> 4;
+  const int wy = wave >> 1, wx = wave & 1;
+  const int K = a.d_in, N = a.d_out;
+  const int nst = (K + C::KC - 1) / C::KC, nst2 = (nst + 1) & ~1;
+
+  // ---- tiles.  Lane l keeps the number of tiles before and up to the end of
+  // the keys KPL l .. KPL l + KPL - 1.
+  int before, upto;
+  {
+    int cnt = 0, off[KPL + 1];
+#pragma unroll
+    for (int i = 0; i <= KPL; ++i) off[i] = a.offsets[min(lane * KPL + i, a.E)];
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) cnt += (off[i + 1] - off[i] + C::BM - 1) / C::BM * a.nt;
+    upto = cnt;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += v;
+    }
+    before = upto - cnt;
+  }
+  const int n_tiles = __builtin_amdgcn_readfirstlane(__shfl(upto, 63, 64));
+  const int per_xcd = (n_tiles + kXcds - 1) / kXcds;
+  const int xcd = blockIdx.x % kXcds, step = gridDim.x / kXcds;
+  int tile = xcd * per_xcd + blockIdx.x / kXcds;
+  const int tile_end = min((xcd + 1) * per_xcd, n_tiles);
+  if (tile >= tile_end) return;
+
+  struct Tile {
+    int e, n0, u0, hi;   // expert, first column, first row, end of the expert's rows
+  };
+  // (offsets through the constant address space: scalar loads, which the copies
+  // in flight do not hold up); within an expert, groups of up to eight row tiles
+  // walk the columns together
+  const auto soff = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.offsets;
+  auto locate = [&](int t) {
+    const int owner = __builtin_ctzll(__ballot(t >= before && t < upto));
+    int rem = t - __builtin_amdgcn_readlane(before, owner), q = owner * KPL;
+    int lo = soff[q], hi = soff[min(q + 1, a.E)];
+    for (;;) {   // at most KPL keys
+      const int n = (hi - lo + C::BM - 1) / C::BM * a.nt;
+      if (rem < n) break;
+      rem -= n;
+      ++q;
+      lo = hi;
+      hi = soff[min(q + 1, a.E)];
+    }
+    const int m_e = (hi - lo + C::BM - 1) / C::BM;
+    const int grp = rem / (kRowGroup * a.nt), gsz = min(kRowGroup, m_e - grp * kRowGroup);
+    const int ing = rem - grp * kRowGroup * a.nt;
+    return Tile{q, ing / gsz * C::BN, lo + (grp * kRowGroup + ing % gsz) * C::BM, hi};
+  };
+  // pairs of the wave's rows 128 wy + lane and + 64 (past the segment: its last)
+  auto pairs = [&](const Tile& t, int (&p)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p[i] = a.pair_list[min(t.u0 + 128 * wy + 64 * i + lane, t.hi - 1)];
+  };
+  Tile cur = locate(tile), nxt = cur;
+  int pc[2], pn[2];      // pairs of the current and the next tile
+  pairs(cur, pc);
+  bool more = tile + step < tile_end;
+  if (more) nxt = locate(tile + step);
+  pairs(nxt, pn);
+
+  // ---- copies: the waves wx = 0 copy the x rows of their wy, the others the W
+  // columns of the half wy: of a slot eight 8-row copies, lane l the chunk at
+  // position l & 7 of row l >> 3.  Offsets count 16-byte chunks.
+  const int crl = lane >> 3, cpos = lane & 7;
+  const bool xwave = wx == 0;
+  const int col[2] = {cpos ^ l_swz(crl), cpos ^ l_swz(8 + crl)};
+  uint32_t roff[2][NC];    // slots P[v] of even and of odd v
+  const char* base;        // x, or the tile's first column of W_e
+  auto set_tile = [&](const Tile& t, const int (&p)[2]) {
+    base = xwave ? static_cast<const char*>(a.x)
+                 : static_cast<const char*>(a.W) + ((size_t)t.e * K * N + t.n0) * 2;
+#pragma unroll
+    for (int par = 0; par < 2; ++par)
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const int h = xwave ? 1 - par : par;   // x unit v + 1, W unit v + 2
+        const int c = 16 * wy + 8 * h + (cpos ^ lt_swz(8 * i + crl));
+        const uint32_t w = (uint32_t)(8 * i + crl) * (uint32_t)(N / 8) + min(c, (N - t.n0) / 8 - 1);
+        const uint32_t x = (uint32_t)__shfl(p[h], 8 * i + crl, 64) * (uint32_t)(K / 8);
+        roff[par][i] = xwave ? x : w;
+      }
+  };
+  set_tile(cur, pc);
+  const uint32_t cbase = lds_addr(smem) + (xwave ? 0 : C::UNIT) + wy * (C::UNIT / 2);
+  uint32_t cslot = cbase;      // where this wave's copies of the next slot go
+  int cst = -1;                // stage that this wave copies (x starts half a stage early)
+  const char* sbase = base;    // of that stage
+  uint32_t colb[2] = {0, 0};   // x: chunk of the lane's column, by copy parity
+  int wgroups = 8;             // W: 8-row groups of the stage inside the contraction
+  // ENDS: the stage may be the first one past the tile (then it is the next
+  // tile's first, or the last one again)
+  auto begin_copies = [&](int par, bool ends) {
+    if (par == (xwave ? 1 : 0)) ++cst;
+    if (ends && cst == nst2) {
+      cst = more ? 0 : nst2 - 1;
+      if (more) set_tile(nxt, pn);
+    }
+    const int st = max(0, min(cst, nst - 1));
+    if (xwave) {
+      sbase = base;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) colb[c] = min(st * (C::KC / 8) + col[c], K / 8 - 1);
+    } else {
+      sbase = base + (size_t)st * (C::KC * 2) * N;
+      if (RAGGED) wgroups = min(8, K / 8 - 8 * st);
+    }
+  };
+  auto copy = [&](int par, int i) {
+    // W groups past the contraction repeat its last one
+    const char* b = RAGGED ? sbase + (ptrdiff_t)(min(i, wgroups - 1) - i) * 16 * N : sbase;
+    dma16(b + (size_t)(roff[par][i] + colb[i & 1]) * 16, __builtin_amdgcn_readfirstlane(cslot + i * 1024));
+  };
+  auto end_copies = [&]() {
+    cslot += C::SLOT;
+    if (cslot >= cbase + C::SLOTS * C::SLOT) cslot = cbase;
+  };
+#pragma unroll
+  for (int v = -2; v < 2; ++v) {
+    begin_copies(v & 1, false);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) copy(v & 1, i);
+    end_copies();
+  }
+
+  F x0[4], x1a[4], x1b[4], wa[16], wb[16];   // x: K-block 0 and 1 of a half, W: [nb + 8 kh]
+  f32x4 acc[8][8];
+#pragma unroll
+  for (int nb = 0; nb < 8; ++nb)
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // ---- fragment reads.  x rows 64 wy + 16 mb + c16 of a unit, as in the
+  // forward.  W fragment nb of K-block kh: 8 bytes of the rows 32 kh + 8 g + 4 h +
+  // (c16 >> 2) of the unit's wx half, at chunk 2 nb + (c16 & 3) / 2; the swizzle
+  // depends on the lane only, and moves nb.
+  const int xl = (64 * wy + c16) * ROWB + ((g ^ l_swz(c16)) << 4);
+  int wtl[4];
+#pragma unroll
+  for (int nb = 0; nb < 4; ++nb) {
+    const int r = 8 * g + (c16 >> 2);
+    wtl[nb] = C::UNIT + (64 * wx + r) * ROWB + (((2 * nb + ((c16 & 3) >> 1)) ^ lt_swz(r)) << 4) + ((c16 & 1) << 3);
+  }
+  int rslot = 0;     // slot that the half-step reads
+  auto wt_read = [&](int nb, int kh) {
+    s16x4 h2[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      h2[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(smem + rslot + wtl[nb] + (32 * kh + 4 * h) * ROWB));
+    return __builtin_bit_cast(F, __builtin_shufflevector(h2[0], h2[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // Half-step h = PAR of stage st: matrix work on (x0, xc, wc) for the wave's row
+  // blocks 4 h .. 4 h + 3; reads the next half's x fragments and half of the next
+  // stage's W fragments; copies the slot after next but three.
+  // The copies come to the end of the tile in its last stage but two, an odd one.
+  // drained: the first four half-steps behind a tile whose 32 stores were all
+  // issued.  The slots they read were copied before the stores, which may all be
+  // under way.  (Any other order has 24 copies behind the needed ones.)
+  auto half = [&](auto par_c, auto mma_c, auto odd_c, int st, bool drained, F (&x1)[4], F (&wc)[16], F (&x1n)[4], F (&wn)[16]) {
+    constexpr int PAR = decltype(par_c)::value;
+    constexpr bool MMA = decltype(mma_c)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    if (drained) wait_vmcnt<32>();
+    else wait_vmcnt<24>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    const char* xs = smem + rslot + xl;
+    const char* xs1 = smem + rslot + (xl ^ 64);
+    begin_copies(PAR, decltype(odd_c)::value);
+    const int c = st * C::KC + 8 * g;
+    const bool past = RAGGED && MMA && st * C::KC + C::KC > K;   // wave-uniform
+    if (PAR == 0 && past) {
+#pragma unroll
+      for (int nb = 0; nb < 8; ++nb) {
+        if (c >= K) wc[nb] = Tr<__bf16>::zero();
+        if (c + 32 >= K) wc[nb + 8] = Tr<__bf16>::zero();
+      }
+    }
+    if (past) {
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb) {
+        if (c >= K) x0[mb] = Tr<__bf16>::zero();
+        if (c + 32 >= K) x1[mb] = Tr<__bf16>::zero();
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i < 8) {
+        if (i < 4) x1n[i] = *reinterpret_cast<const F*>(xs1 + i * 16 * ROWB);
+        wn[4 * PAR + (i & 3) + 8 * (i >> 2)] = wt_read(i & 3, i >> 2);
+        copy(PAR, i);
+      }
+      if (i >= 8 && i < 12) x0[i - 8] = *reinterpret_cast<const F*>(xs + (i - 8) * 16 * ROWB);
+      if constexpr (MMA) {
+#pragma unroll
+        for (int mb = 0; mb < 4; ++mb) {
+          const int nb = i & 7, kh = i >> 3;
+          mfma_acc(acc[nb][4 * PAR + mb], wc[nb + 8 * kh], kh ? x1[mb] : x0[mb]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    end_copies();
+    rslot = rslot == (C::SLOTS - 1) * C::SLOT ? 0 : rslot + C::SLOT;
+  };
+  using P0 = std::integral_constant<int, 0>;
+  using P1 = std::integral_constant<int, 1>;
+  using Yes = std::true_type;
+  using No = std::false_type;
+  __bf16* Y = static_cast<__bf16*>(a.y);
+  half(P0{}, No{}, No{}, 0, false, x1a, wb, x1b, wa);
+  half(P1{}, No{}, No{}, 0, false, x1b, wb, x1a, wa);
+  bool drained = false;
+  for (;;) {
+    for (int st = 0; st < nst2; st += 2) {   // two stages: the W fragments change registers
+      half(P0{}, Yes{}, No{}, st, drained, x1a, wa, x1b, wb);
+      half(P1{}, Yes{}, No{}, st, drained, x1b, wa, x1a, wb);
+      half(P0{}, Yes{}, Yes{}, st + 1, drained, x1a, wb, x1b, wa);
+      half(P1{}, Yes{}, Yes{}, st + 1, drained, x1b, wb, x1a, wa);
+      drained = false;
+    }
+    // ---- the tile after next, then this tile's results: lane (c16, g) holds
+    const bool last = !more;
+    Tile nn = nxt;
+    int pnn[2];
+    tile += step;
+    more = tile + step < tile_end;
+    if (more) nn = locate(tile + step);
+    pairs(nn, pnn);
+    mfma_done();
+    __builtin_amdgcn_sched_barrier(0);
+    // columns 4 g .. 4 g + 3 of a 16-column block of row c16.  Of two neighbouring
+    // blocks the lanes of a row trade their 8-byte pieces until lane g holds the
+    // 16 bytes g: a store covers 64 bytes of each of 16 rows (32 bytes of them:
+    // 35 us more for 134 MB of results).
+    const int col0 = cur.n0 + 128 * wx + 8 * g;
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nb = 0; nb < 8; ++nb) asm volatile("" : "+a"(acc[nb][mb]));   // read behind mfma_done
+      u32x4 o[4];
+#pragma unroll
+      for (int nb = 0; nb < 8; nb += 2) {
+        u32x2 lo = round4(acc[nb][mb]), hi = round4(acc[nb + 1][mb]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          u32x2 s = __builtin_amdgcn_permlane32_swap(lo[i], hi[i], false, false);
+          s = __builtin_amdgcn_permlane16_swap(s[0], s[1], false, false);
+          o[nb / 2][i] = s[0];
+          o[nb / 2][2 + i] = s[1];
+        }
+      }
+      const int p = __shfl(pc[mb >> 2], 16 * (mb & 3) + c16, 64);
+      if (cur.u0 + 128 * wy + 16 * mb + c16 < cur.hi) {
+        __bf16* row = Y + (size_t)p * N + col0;
+#pragma unroll
+        for (int nb = 0; nb < 8; nb += 2)
+          if (col0 + 16 * nb < N) *reinterpret_cast<u32x4*>(row + 16 * nb) = o[nb / 2];
+      }
+#pragma unroll
+      for (int nb = 0; nb < 8; ++nb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (last) break;
+    // the loads above are older than the stores: a use here waits for them only,
+    // one further on would wait for the copies as well
+    asm volatile("" : "+v"(pnn[0]), "+v"(pnn[1]));
+    drained = cur.u0 + C::BM <= cur.hi && cur.n0 + C::BN <= N;
+    cur = nxt;
+    nxt = nn;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      pc[i] = pn[i];
+      pn[i] = pnn[i];
+    }
+  }
+  wait_vmcnt<0>();   // copies past the last tile (repeats of its last stage)
+}

@@ -393,11 +393,6 @@ struct Large {
 // consecutive rows, and any 8 even or odd rows among 16, take 8 positions.
 __device__ inline int l_swz(int row) { return (row & 7) ^ ((row >> 3) & 1); }
 
-// The same of a 128-byte W^T row (DX): pairs of chunks trade places, so that the
-// 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread
-// over the banks for the lanes of one g and of two.
-__device__ inline int lt_swz(int r) { return 2 * ((r & 3) ^ ((r >> 3) & 1)); }
-
 // Key of a tile when key q owns ceil(rows / BM) * per tiles, key-major: its
 // segment [lo, hi) and the tile's index among the key's tiles (wave-level,
 // every lane gets the result; false past the last tile).
@@ -449,10 +444,7 @@ __device__ inline bool locate_key(const int32_t* offsets, int n_keys, int BM, in
 // WIDE: x of 4 GiB or more (below 64 GiB): the copies' 32-bit offsets count
 // 16-byte chunks instead of bytes (300,000 rows of 8192 through 8 experts of
 // 1024 columns: 5.27 ms; the medium tiles 6.57).
-// DX (W^T): a W unit is 64 contraction rows of 64 columns for each wx, so a
-// copy's rows are the stage's and the fragments are transposed reads (two of 8
-// bytes in the place of one of 16).
-template <bool RAGGED, bool WIDE, bool DX>
+template <bool RAGGED, bool WIDE>
 __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeArgs a) {
   using C = Large;
   using F = bf16x8;
@@ -495,10 +487,9 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
   // registers ahead of the copies: loads return in order, so behind them each
   // step of the chain pair -> h row -> h would wait for copies from HBM
   F x0[4], x1a[4], x1b[4], wa[16], wb[16];   // x: K-block 0 and 1 of a half, W: [nb + 8 kh]
-  const bool adapted = !DX && a.H;
-  const int q = adapted ? a.key_of[e] : 0;
-  const int r_q = adapted ? a.keys.rank[q] : 0;
-  const __bf16* Bq = static_cast<const __bf16*>(a.B) + (adapted ? (size_t)d_out * a.keys.roff[q] : 0);
+  const int q = a.H ? a.key_of[e] : 0;
+  const int r_q = a.H ? a.keys.rank[q] : 0;
+  const __bf16* Bq = static_cast<const __bf16*>(a.B) + (a.H ? (size_t)d_out * a.keys.roff[q] : 0);
   const __bf16* Hm = static_cast<const __bf16*>(a.H);
   const bool bvec = (r_q & 7) == 0;
   int hrow[8];
@@ -527,13 +518,10 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
   // 64 rows, lane l the chunk at position l & 7 of row l >> 3.  Rows are
   // offsets (OU) from x or from the tile's first W row; chunks past d_in repeat the
   // row's last one (masked in the fragments of a ragged d_in).
-  // DX: the W rows are the eighths of a stage's 64 contraction rows, 64 of the
-  // wave's columns each (chunks past d_out repeat the last one); their offsets
-  // do not move with the stage, the base does.
   const int crl = lane >> 3, cpos = lane & 7;
   const bool xwave = wave < 2;
   const char* base = xwave ? reinterpret_cast<const char*>(X)
-                           : reinterpret_cast<const char*>(DX ? Wt + n0 : Wt + (size_t)n0 * d_in);
+                           : reinterpret_cast<const char*>(Wt + (size_t)n0 * d_in);
   uint32_t roff[2][NC];   // slots P[v] of even and of odd v
 #pragma unroll
   for (int par = 0; par < 2; ++par)
@@ -542,11 +530,6 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
       const int h = xwave ? 1 - par : par;   // x unit v + 1, W unit v + 2
       const int row = 128 * (wave & 1) + 64 * h + 8 * i + crl;
       int src;
-      if (DX && !xwave) {
-        const int c = 128 * (wave & 1) + 64 * h + 8 * (cpos ^ lt_swz(8 * i + crl));
-        roff[par][i] = (uint32_t)(8 * i + crl) * (uint32_t)(2 * d_out / OU) + 2 * min(c, d_out - 8 - n0) / OU;
-        continue;
-      }
       if (xwave) {
         const int uc = min(u0 + row, hi - 1);
         src = a.per_pair ? pair_of(uc) : a.row_token[uc];
@@ -560,23 +543,13 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
   const uint32_t cbase = lds_addr(smem) + (xwave ? 0 : C::UNIT) + (wave & 1) * (C::UNIT / 2);
   uint32_t cslot = cbase;             // where this wave's copies of the next slot go
   uint32_t colb[2];                   // column (OU) of a lane's chunk, by copy parity
-  const char* sbase = base;           // of the slot's stage (DX: W)
-  int wgroups = 8;                    // 8-row groups of that stage inside the contraction
   auto begin_copies = [&](int v) {    // of slot P[v]
     const int st = max(0, min((v + (xwave ? 1 : 2)) >> 1, nst - 1));
-    if (DX && !xwave) {
-      sbase = base + (size_t)st * C::KC * 2 * d_out;
-      if (RAGGED) wgroups = min(8, d_in / 8 - 8 * st);
-      colb[0] = colb[1] = 0;
-      return;
-    }
 #pragma unroll
     for (int c = 0; c < 2; ++c) colb[c] = 2 * min(st * C::KC + col[c], d_in - 8) / OU;
   };
   auto copy = [&](int par, int i) {
-    const char* p = (DX ? sbase : base) + (size_t)(roff[par][i] + colb[i & 1]) * OU;
-    // groups past the contraction repeat its last one
-    if (DX && RAGGED && !xwave && i >= wgroups) p -= (size_t)(i - wgroups + 1) * 16 * d_out;
+    const char* p = base + (size_t)(roff[par][i] + colb[i & 1]) * OU;
     dma16(p, __builtin_amdgcn_readfirstlane(cslot + i * 1024));
   };
   auto end_copies = [&]() {
@@ -619,22 +592,6 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
   const int xl = (64 * wy + c16) * ROWB + ((g ^ l_swz(c16)) << 4);
   const int wl = C::UNIT + (64 * wx + c16) * ROWB + ((g ^ l_swz(c16)) << 4);
   int rslot = 0;                      // slot that the half-step reads
-  // DX: fragment nb of K-block kh reads 8 bytes of the rows 32 kh + 8 g + 4 h +
-  // (c16 >> 2) of the unit's wx half, at chunk 2 nb + (c16 & 3) / 2: the
-  // swizzle depends on the lane only, and moves nb.
-  int wtl[4];
-#pragma unroll
-  for (int nb = 0; nb < 4; ++nb) {
-    const int r = 8 * g + (c16 >> 2);
-    wtl[nb] = C::UNIT + 64 * wx * ROWB + r * ROWB + (((2 * nb + ((c16 & 3) >> 1)) ^ lt_swz(r)) << 4) + ((c16 & 1) << 3);
-  }
-  auto wt_read = [&](int nb, int kh) {
-    s16x4 h2[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      h2[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(smem + rslot + wtl[nb] + (32 * kh + 4 * h) * ROWB));
-    return __builtin_bit_cast(F, __builtin_shufflevector(h2[0], h2[1], 0, 1, 2, 3, 4, 5, 6, 7));
-  };
   // Half-step v = 2 st + h (h = PAR): matrix work on (xc, wc) for the wave's
   // row blocks 4 h .. 4 h + 3; reads slot P[v]: the next half's x fragments
   // into xn, the W fragments nb = 4 h .. 4 h + 3 of stage st + 1 into wn;
@@ -676,9 +633,8 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
     for (int i = 0; i < 16; ++i) {
       if (i < 8) {   // groups 0..7 work on K-block 0, groups 8..15 on K-block 1
         if (i < 4) x1n[i] = *reinterpret_cast<const F*>(xs1 + i * 16 * ROWB);
-        F& wf = wn[4 * PAR + (i & 3) + 8 * (i >> 2)];
-        if constexpr (DX) wf = wt_read(i & 3, i >> 2);
-        else wf = *reinterpret_cast<const F*>((i < 4 ? ws : ws1) + (i & 3) * 16 * ROWB);
+        wn[4 * PAR + (i & 3) + 8 * (i >> 2)] =
+            *reinterpret_cast<const F*>((i < 4 ? ws : ws1) + (i & 3) * 16 * ROWB);
         copy(PAR, i);
       }
       if (i >= 8 && i < 12) x0[i - 8] = *reinterpret_cast<const F*>(xs + (i - 8) * 16 * ROWB);
@@ -739,6 +695,8 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
     }
   }
 }
+
+#include "moe_dx.hpp"
 
 // ---------------------------------------------------------------- few rows per expert
 //
@@ -908,17 +866,27 @@ hipError_t launch_moe_mid(MoeArgs a, long P, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <bool DX = false>
 hipError_t launch_moe_large(MoeArgs a, long P, bool wide, hipStream_t stream) {
   a.nt = (a.d_out + Large::BN - 1) / Large::BN;
   const long max_tiles = ((P + Large::BM - 1) / Large::BM + a.E) * a.nt;
   const long grid = (max_tiles + kXcds - 1) / kXcds * kXcds;
   if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
   const bool ragged = a.d_in % (2 * Large::KC) != 0;
-  if (wide && ragged) moe_gemm_large_kernel<true, true, DX><<<(int)grid, Large::THREADS, 0, stream>>>(a);
-  else if (wide) moe_gemm_large_kernel<false, true, DX><<<(int)grid, Large::THREADS, 0, stream>>>(a);
-  else if (ragged) moe_gemm_large_kernel<true, false, DX><<<(int)grid, Large::THREADS, 0, stream>>>(a);
-  else moe_gemm_large_kernel<false, false, DX><<<(int)grid, Large::THREADS, 0, stream>>>(a);
+  if (wide && ragged) moe_gemm_large_kernel<true, true><<<(int)grid, Large::THREADS, 0, stream>>>(a);
+  else if (wide) moe_gemm_large_kernel<false, true><<<(int)grid, Large::THREADS, 0, stream>>>(a);
+  else if (ragged) moe_gemm_large_kernel<true, false><<<(int)grid, Large::THREADS, 0, stream>>>(a);
+  else moe_gemm_large_kernel<false, false><<<(int)grid, Large::THREADS, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_moe_dx_large(MoeArgs a, long P, hipStream_t stream) {
+  a.nt = (a.d_out + Large::BN - 1) / Large::BN;
+  const long max_tiles = ((P + Large::BM - 1) / Large::BM + a.E) * a.nt;
+  if (max_tiles > 0x7fffffffL - 4096) return hipErrorInvalidConfiguration;
+  // one block per CU, the same number for each XCD
+  const int cus = (device_cu_count() + kXcds - 1) / kXcds * kXcds;
+  if (a.d_in % (2 * Large::KC) != 0) moe_dx_large_kernel<true><<<cus, Large::THREADS, 0, stream>>>(a);
+  else moe_dx_large_kernel<false><<<cus, Large::THREADS, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -980,7 +948,7 @@ bool mid_f32(const MoeArgs& a, long P) {
 
 hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream) {
   if (dtype == ACE_F32) return launch_moe_mid<float, true>(a, P, stream);
-  if (P >= kLargeRows * a.E) return launch_moe_large<true>(a, P, 2 * P * a.d_in >= (1L << 32), stream);
+  if (P >= kLargeRows * a.E && a.d_in >= kDxLargeK) return launch_moe_dx_large(a, P, stream);
   return launch_moe_mid<__bf16, true>(a, P, stream);
 }
 
