@@ -20,6 +20,42 @@
 // over the banks for the lanes of one g and of two.
 __device__ inline int lt_swz(int r) { return 2 * ((r & 3) ^ ((r >> 3) & 1)); }
 
+// Fragments of W^T.  A stage holds contraction rows of BN columns; fragment:
+// columns n .. n + 15 (lane c16), contraction rows PER*g .. PER*g + PER - 1 of a
+// K-block (lane group g), as in Tr<T>::frag.
+// bf16: ds_read_b64_tr_b16 hands lane i of 16 the element i & 3 of the 8 bytes
+// that lanes 4 j + (i >> 2), j = 0..3, address.  fp32: four words of four rows.
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Chunk swizzle of a row of 256 bytes and more (lt_swz for those of 128): bf16
+// spreads the rows 8 g + (0..3) of a transposed read, fp32 the rows 4 g + i.
+template <typename T, int BN>
+__device__ inline int wt_swz(int r) {
+  if (sizeof(T) == 4) return 4 * ((r >> 2) & 3);
+  return BN == 64 ? lt_swz(r) : 2 * ((r & 3) | (((r >> 3) & 1) << 2));
+}
+
+template <typename T, int BN>
+__device__ inline typename Tr<T>::frag wt_frag(const char* S, int n, int lane) {
+  constexpr int ROWB = BN * (int)sizeof(T);
+  const int c16 = lane & 15, g = lane >> 4;
+  if constexpr (sizeof(T) == 2) {
+    const int r = 8 * g + (c16 >> 2);   // and 4 on: the same swizzle
+    const char* p = S + r * ROWB + ((((n >> 3) + ((c16 & 3) >> 1)) ^ wt_swz<T, BN>(r)) << 4) + ((c16 & 1) << 3);
+    s16x4 h2[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) h2[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * h * ROWB));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h2[0], h2[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    const char* p = S + 4 * g * ROWB + ((((n >> 2) + (c16 >> 2)) ^ wt_swz<T, BN>(4 * g)) << 4) + ((c16 & 3) << 2);
+    f32x4 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = *reinterpret_cast<const float*>(p + i * ROWB);
+    return f;
+  }
+}
+
 // Four values rounded to bf16, as two words.
 __device__ inline u32x2 round4(f32x4 v) {
   return __builtin_bit_cast(u32x2, bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]});
@@ -322,4 +358,221 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
     }
   }
   wait_vmcnt<0>();   // copies past the last tile (repeats of its last stage)
+}
+
+// ---- few rows per expert: the weights bound the call, and a block streams them.
+//
+// A block takes up to 16 NRB rows of one expert and BN columns (256 bytes of a W
+// row).  Its four waves split the contraction: wave w takes the K-blocks w, w +
+// 4, ..., each through a ring of its own in LDS (the K-block's W rows and the same
+// columns of the x rows), so no barrier stands in the loop; the four sums meet in
+// LDS at the end, in wave order.  A third buffer per wave gained nothing (fewer
+// streams at a time serve HBM better).  64 experts of 2048 x 1024 with 4 rows
+// each: 44 us, 5.9 TB/s of weights.
+template <typename T, int NRB, int BN_>
+struct DxStream {
+  static constexpr int KB = Tr<T>::KB, BM = 16 * NRB, BN = BN_, NBUF = 2, NCB = BN / 16;
+  static constexpr int WBYTES = KB * BN * (int)sizeof(T), STAGE = WBYTES + BM * kGRowBytes;
+  static constexpr int NS = WBYTES / 1024;                  // W copies of a stage
+  static constexpr int WCH = BN * (int)sizeof(T) / 16;      // chunks of a W row
+  static constexpr int CST = BN + 4;                        // row stride of the sums
+  static constexpr int RING = 4 * NBUF * STAGE, SUMS = 4 * BM * CST * 4;
+};
+
+template <typename T, int NRB, int BN>
+__global__ __launch_bounds__(256) void moe_dx_stream_kernel(MoeArgs a) {
+  using C = DxStream<T, NRB, BN>;
+  using F = typename Tr<T>::frag;
+  constexpr int PER = Tr<T>::PER, KB = C::KB, NCB = C::NCB, NBUF = C::NBUF;
+  __shared__ __attribute__((aligned(16))) char smem[C::RING > C::SUMS ? C::RING : C::SUMS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, g = lane >> 4;
+  const int mt = blockIdx.x / a.nt, n0 = (blockIdx.x % a.nt) * C::BN;
+  int e, u0, u_end;
+  if (!locate_tile(a.offsets, a.E, C::BM, mt, &e, &u0, &u_end)) return;   // block-uniform
+  e = __builtin_amdgcn_readfirstlane(e);
+  const int K = a.d_in, N = a.d_out;
+  const T* X = static_cast<const T*>(a.x);
+  const T* Wt = static_cast<const T*>(a.W) + (size_t)e * K * N + n0;
+  // x copies: lane l takes the chunk at position l & 3 of row l >> 2 of 16; only
+  // those that hold rows of the tile
+  const int nx = __builtin_amdgcn_readfirstlane(min(NRB, (u_end - u0 + 15) / 16));
+  const T* xsrc[NRB];
+#pragma unroll
+  for (int i = 0; i < NRB; ++i)
+    xsrc[i] = X + (size_t)a.pair_list[min(u0 + 16 * i + (lane >> 2), u_end - 1)] * K;
+  const int xcol = PER * ((lane & 3) ^ g_swz(lane >> 2));
+  // W copies: 64 chunks each, of rows of WCH
+  const int wrow = lane / C::WCH;
+  constexpr int RPC = 64 / C::WCH;
+  auto col_of = [&](int i) { return min(PER * ((lane % C::WCH) ^ wt_swz<T, BN>(RPC * i + wrow)), N - PER - n0); };
+  const int nst = (K + KB - 1) / KB;
+  const int mine = (nst - wave + 3) / 4;    // K-blocks of this wave
+  char* ring = smem + wave * NBUF * C::STAGE;
+  auto issue = [&](int i) {
+    const int k0 = (wave + 4 * i) * KB;
+    const uint32_t buf = lds_addr(ring) + (i % NBUF) * C::STAGE;
+    const T* Wk = Wt + (size_t)k0 * N;
+#pragma unroll
+    for (int c = 0; c < C::NS; ++c) {
+      const int col = col_of(c);
+      const int row = min(RPC * c + wrow, K - 1 - k0);
+      dma16_nt(Wk + ((uint32_t)row * (uint32_t)N + (uint32_t)col), __builtin_amdgcn_readfirstlane(buf + c * 1024));
+    }
+#pragma unroll
+    for (int r = 0; r < NRB; ++r)
+      if (r < nx)
+        dma16(xsrc[r] + min(k0 + xcol, K - PER), __builtin_amdgcn_readfirstlane(buf + C::WBYTES + r * 1024));
+  };
+  f32x4 acc[NCB][NRB];
+#pragma unroll
+  for (int nb = 0; nb < NCB; ++nb)
+#pragma unroll
+    for (int ib = 0; ib < NRB; ++ib) acc[nb][ib] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < NBUF - 1; ++i)
+    if (i < mine) issue(i);
+  for (int i = 0; i < mine; ++i) {
+    // K-block i - 1 is in registers: its buffer takes K-block i + NBUF - 1
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    if (i + NBUF - 1 < mine) issue(i + NBUF - 1);
+    wait_vmcnt_upto<(NBUF - 1) * (C::NS + NRB)>(min(NBUF - 1, mine - 1 - i) * (C::NS + nx));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    const char* S = ring + (i % NBUF) * C::STAGE;
+    const bool past = (wave + 4 * i) * KB + PER * g >= K;
+    F wf[NCB], xf[NRB];
+#pragma unroll
+    for (int nb = 0; nb < NCB; ++nb) {
+      wf[nb] = wt_frag<T, BN>(S, 16 * nb, lane);
+      if (past) wf[nb] = Tr<T>::zero();
+    }
+#pragma unroll
+    for (int ib = 0; ib < NRB; ++ib) {
+      xf[ib] = *reinterpret_cast<const F*>(S + C::WBYTES + (16 * ib + c16) * kGRowBytes + ((g ^ g_swz(c16)) << 4));
+      if (past || ib >= nx) xf[ib] = Tr<T>::zero();
+    }
+#pragma unroll
+    for (int ib = 0; ib < NRB; ++ib)
+#pragma unroll
+      for (int nb = 0; nb < NCB; ++nb) acc[nb][ib] = Tr<T>::mma(wf[nb], xf[ib], acc[nb][ib]);   // D[column][row]
+  }
+  // ---- the waves' sums
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int ib = 0; ib < NRB; ++ib)
+#pragma unroll
+    for (int nb = 0; nb < NCB; ++nb)
+      *reinterpret_cast<f32x4*>(sums + (wave * C::BM + 16 * ib + c16) * C::CST + 16 * nb + 4 * g) = acc[nb][ib];
+  __syncthreads();
+  typedef __attribute__((ext_vector_type(4))) T T4;
+  T* Y = static_cast<T*>(a.y);
+#pragma unroll
+  for (int i = 0; i < NRB * BN / 64; ++i) {
+    const int it = 256 * i + threadIdx.x, row = it / (BN / 4), col = 4 * (it % (BN / 4));
+    f32x4 v = *reinterpret_cast<const f32x4*>(sums + row * C::CST + col);
+#pragma unroll
+    for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * C::BM + row) * C::CST + col);
+    if (u0 + row < u_end && n0 + col < N)
+      *reinterpret_cast<T4*>(Y + (size_t)a.pair_list[u0 + row] * N + n0 + col) = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+  }
+}
+
+// ---- fp32, many rows per expert: tiles of 128 rows x 128 columns, four waves of
+// 64 x 64, K-blocks of 16 in a ring of three in LDS (48 KB, three blocks per CU:
+// while one waits or stores, the others use the matrix units, which bound the
+// call).  Tile order as in the large bf16 tiles.
+struct DxTile {
+  static constexpr int KB = 16, BM = 128, BN = 128, NBUF = 3;
+  static constexpr int XBYTES = BM * kGRowBytes, STAGE = XBYTES + KB * BN * 4, COPIES = 2;
+};
+
+__global__ __launch_bounds__(256, 3) void moe_dx_tile_kernel(MoeArgs a) {
+  using C = DxTile;
+  using F = f32x4;
+  __shared__ __attribute__((aligned(16))) char smem[C::NBUF * C::STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, g = lane >> 4;
+  const int wy = wave >> 1, wx = wave & 1;
+  const int n_tiles = count_tiles(a.offsets, a.E, C::BM) * a.nt;
+  const int per_xcd = (n_tiles + kXcds - 1) / kXcds;
+  const int bi = blockIdx.x / kXcds;
+  const int tile = (blockIdx.x % kXcds) * per_xcd + bi;
+  if (bi >= per_xcd || tile >= n_tiles) return;
+  int e, lo, hi, rem;
+  if (!locate_key(a.offsets, a.E, C::BM, a.nt, tile, &e, &lo, &hi, &rem)) return;
+  const int m_e = (hi - lo + C::BM - 1) / C::BM;
+  const int grp = rem / (kRowGroup * a.nt), gsz = min(kRowGroup, m_e - grp * kRowGroup);
+  const int ing = rem - grp * kRowGroup * a.nt;
+  const int n0 = ing / gsz * C::BN;
+  const int u0 = lo + (grp * kRowGroup + ing % gsz) * C::BM;
+  const int K = a.d_in, N = a.d_out;
+  const float* X = static_cast<const float*>(a.x);
+  const float* Wt = static_cast<const float*>(a.W) + (size_t)e * K * N + n0;
+  // copies of wave w: x rows 32 w + 16 i + (lane >> 2), W rows 4 w + 2 i + (lane >> 5)
+  const float* xsrc[C::COPIES];
+  int wcol[C::COPIES];
+#pragma unroll
+  for (int i = 0; i < C::COPIES; ++i) {
+    xsrc[i] = X + (size_t)a.pair_list[min(u0 + 32 * wave + 16 * i + (lane >> 2), hi - 1)] * K;
+    wcol[i] = min(4 * ((lane & 31) ^ wt_swz<float, C::BN>(4 * wave + 2 * i + (lane >> 5))), N - 4 - n0);
+  }
+  const int xcol = 4 * ((lane & 3) ^ g_swz(lane >> 2));
+  const int nst = (K + C::KB - 1) / C::KB;
+  const uint32_t sbase = lds_addr(smem);
+  auto issue = [&](int st) {
+    const uint32_t buf = sbase + (st % C::NBUF) * C::STAGE;
+    const int k0 = st * C::KB;
+    const float* Wk = Wt + (size_t)k0 * N;
+#pragma unroll
+    for (int i = 0; i < C::COPIES; ++i) {
+      dma16(xsrc[i] + min(k0 + xcol, K - 4), __builtin_amdgcn_readfirstlane(buf + (32 * wave + 16 * i) * kGRowBytes));
+      const int row = min(4 * wave + 2 * i + (lane >> 5), K - 1 - k0);
+      dma16(Wk + ((uint32_t)row * (uint32_t)N + (uint32_t)wcol[i]),
+            __builtin_amdgcn_readfirstlane(buf + C::XBYTES + (4 * wave + 2 * i) * C::BN * 4));
+    }
+  };
+  f32x4 acc[4][4];
+#pragma unroll
+  for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < C::NBUF - 1; ++s)
+    if (s < nst) issue(s);
+  for (int st = 0; st < nst; ++st) {
+    wait_vmcnt_upto<(C::NBUF - 2) * 2 * C::COPIES>(min(C::NBUF - 2, nst - 1 - st) * 2 * C::COPIES);
+    __syncthreads();
+    if (st + C::NBUF - 1 < nst) issue(st + C::NBUF - 1);
+    const char* S = smem + (st % C::NBUF) * C::STAGE;
+    const bool past = st * C::KB + 4 * g >= K;
+    F xf[4], wf[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      xf[i] = *reinterpret_cast<const F*>(S + (64 * wy + 16 * i + c16) * kGRowBytes + ((g ^ g_swz(c16)) << 4));
+      wf[i] = wt_frag<float, C::BN>(S + C::XBYTES, 64 * wx + 16 * i, lane);
+      if (past) xf[i] = wf[i] = Tr<float>::zero();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)   // the four products of an accumulator block apart
+#pragma unroll
+      for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+        for (int mb = 0; mb < 4; ++mb)   // D[column][row]
+          acc[nb][mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[nb][i], xf[mb][i], acc[nb][mb], 0, 0, 0);
+  }
+  float* Y = static_cast<float*>(a.y);
+  const int col0 = n0 + 64 * wx + 4 * g;
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) {
+    const int u = u0 + 64 * wy + 16 * mb + c16;
+    if (u < hi) {
+      float* row = Y + (size_t)a.pair_list[u] * N + col0;
+#pragma unroll
+      for (int nb = 0; nb < 4; ++nb)
+        if (col0 + 16 * nb < N) *reinterpret_cast<f32x4*>(row + 16 * nb) = acc[nb][mb];
+    }
+  }
 }

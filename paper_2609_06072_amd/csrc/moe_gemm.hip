@@ -46,9 +46,6 @@ struct GCfg {
   static constexpr int BM = 64 * WM, BN = 128 * WN;
   static constexpr int XBYTES = BM * kGRowBytes, STAGE = (BM + BN) * kGRowBytes;
   static constexpr int COPIES = (BM + BN) / 16 / NW;   // 16-row copies per wave per stage
-  // 16-byte chunks of a row of BN columns (DX)
-  template <typename T>
-  static constexpr int wch() { return BN * (int)sizeof(T) / 16; }
   static_assert((BM + BN) / 16 % NW == 0, "copies must split evenly over the waves");
   static_assert(THREADS >= BM, "one thread per tile row fills the row tables");
 };
@@ -91,51 +88,7 @@ __device__ inline int count_tiles(const int32_t* offsets, int n_keys, int BM) {
   return cnt;
 }
 
-// ---- W^T (the input gradient, DX): the contraction runs over W_e's rows, and
-// a stage holds KB of them, row-major, BN columns each.
-//
-// Chunk swizzle of such a row (an XOR on the chunk index).  bf16: a transposed
-// read touches 32 bytes of each of the 16 rows 8 g + (0..3) (+ 4); 8 rows of a
-// half-wave, and the four of 16 lanes, take different banks.  fp32: a read
-// takes 64 bytes of the rows 4 g + i.
-template <typename T>
-__device__ inline int wt_swz(int r) {
-  return sizeof(T) == 2 ? 2 * ((r & 3) | (((r >> 3) & 1) << 2)) : 4 * ((r >> 2) & 3);
-}
-
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-// Fragment of columns n .. n + 15 (lane c16) over the contraction rows r0 ..
-// r0 + KB - 1 of rows of BN columns at S: elements PER*g .. PER*g + PER - 1 of
-// lane group g, as in Tr<T>::frag.  bf16: ds_read_b64_tr_b16 hands lane i of 16
-// the element i & 3 of the 8 bytes that lanes 4 j + (i >> 2), j = 0..3, address.
-template <typename T, int BN>
-__device__ inline typename Tr<T>::frag wt_frag(const char* S, int r0, int n, int lane) {
-  constexpr int ROWB = BN * (int)sizeof(T);
-  const int c16 = lane & 15, g = lane >> 4;
-  if constexpr (sizeof(T) == 2) {
-    s16x4 h2[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = r0 + 8 * g + 4 * h + (c16 >> 2);
-      const int c = (n >> 3) + ((c16 & 3) >> 1);
-      h2[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(S + r * ROWB + ((c ^ wt_swz<T>(r)) << 4) + ((c16 & 1) << 3)));
-    }
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h2[0], h2[1], 0, 1, 2, 3, 4, 5, 6, 7));
-  } else {
-    f32x4 f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + 4 * g + i;
-      const int c = (n >> 2) + (c16 >> 2);
-      f[i] = *reinterpret_cast<const float*>(S + r * ROWB + ((c ^ wt_swz<T>(r)) << 4) + ((c16 & 3) << 2));
-    }
-    return f;
-  }
-}
-
-template <typename T, class C, bool DX>
+template <typename T, class C>
 __global__ __launch_bounds__(C::THREADS, 512 / C::THREADS) void moe_gemm_kernel(MoeArgs a) {
   using F = typename Tr<T>::frag;
   constexpr int PER = Tr<T>::PER, KB = Tr<T>::KB;
@@ -183,7 +136,7 @@ __global__ __launch_bounds__(C::THREADS, 512 / C::THREADS) void moe_gemm_kernel(
   // stored.
   const bool active = u0 + 64 * wy < uend;
   const T* X = static_cast<const T*>(a.x);
-  const T* Wt = static_cast<const T*>(a.W) + (DX ? (size_t)e * a.d_in * a.d_out + n0 : ((size_t)e * a.d_out + n0) * a.d_in);
+  const T* Wt = static_cast<const T*>(a.W) + ((size_t)e * a.d_out + n0) * a.d_in;
   const int d_in = a.d_in, d_out = a.d_out;
   const int nst = (d_in + KB - 1) / KB;
 
@@ -192,35 +145,26 @@ __global__ __launch_bounds__(C::THREADS, 512 / C::THREADS) void moe_gemm_kernel(
   // swizzle only sees bits 1..3 of the row, i.e. of lane >> 2, so one chunk
   // offset serves every copy; rows are 32-bit element offsets from x (fewer
   // than 2^32 elements, see launch_moe_gemm) or from the tile's first W row.
-  // DX: a stage's W rows are its KB contraction indices, wch() chunks of BN
-  // columns each, 64 chunks a copy; their roff is the column, and x's counts
-  // 16-byte chunks (gradient rows may pass 4 GiB).
   const int cpos = lane & 3, crl = lane >> 2;
   const int coff = PER * (cpos ^ g_swz(crl));
-  auto wrow = [&](int blk) { return (64 / C::template wch<T>()) * (blk - BM / 16) + lane / C::template wch<T>(); };
   uint32_t roff[COPIES];
 #pragma unroll
   for (int i = 0; i < COPIES; ++i) {
     const int blk = wave * COPIES + i;        // 16-row copy index over [x rows | W rows]
     const int row = 16 * blk + crl;
-    if (16 * blk < BM) roff[i] = (uint32_t)s_src[row] * (uint32_t)(DX ? d_in / PER : d_in);
-    else if (DX) roff[i] = (uint32_t)min(PER * ((lane % C::template wch<T>()) ^ wt_swz<T>(wrow(blk))), d_out - PER - n0);
-    else roff[i] = (uint32_t)min(row - BM, d_out - 1 - n0) * (uint32_t)d_in;
+    roff[i] = 16 * blk < BM ? (uint32_t)s_src[row] * (uint32_t)d_in
+                            : (uint32_t)min(row - BM, d_out - 1 - n0) * (uint32_t)d_in;
   }
   const uint32_t sbase = lds_addr(smem);
   auto issue = [&](int st) {
     const uint32_t buf = sbase + (st % NBUF) * STAGE;
     const uint32_t kk = (uint32_t)min(st * KB + coff, d_in - PER);
-    const T* Wst = DX ? Wt + (size_t)st * KB * d_out : Wt;
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
       const int blk = wave * COPIES + i;
       const bool xcopy = 16 * blk < BM;
-      const T* src;
-      if (!DX) src = (xcopy ? X : Wt) + (roff[i] + kk);
-      else if (xcopy) src = X + (size_t)(roff[i] + kk / PER) * PER;
-      else src = Wst + (roff[i] + (uint32_t)min(wrow(blk), d_in - 1 - st * KB) * (uint32_t)d_out);
-      dma16(src, __builtin_amdgcn_readfirstlane(buf + 16 * blk * kGRowBytes));
+      dma16((xcopy ? X : Wt) + (roff[i] + kk),
+            __builtin_amdgcn_readfirstlane(buf + 16 * blk * kGRowBytes));
     }
   };
 #pragma unroll
@@ -234,7 +178,7 @@ __global__ __launch_bounds__(C::THREADS, 512 / C::THREADS) void moe_gemm_kernel(
     for (int mb = 0; mb < 4; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // ---- adapter K-blocks: acc[n][m] += sum_rho B_q[n][rho] h_m[rho]
-  if (!DX && a.H && active) {
+  if (a.H && active) {
     const int q = a.key_of[e];
     const int r_q = a.keys.rank[q];
     const T* Bq = static_cast<const T*>(a.B) + (size_t)d_out * a.keys.roff[q];
@@ -273,10 +217,8 @@ __global__ __launch_bounds__(C::THREADS, 512 / C::THREADS) void moe_gemm_kernel(
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb) xf[mb] = *reinterpret_cast<const F*>(S + xl + mb * 16 * kGRowBytes);
 #pragma unroll
-    for (int nb = 0; nb < 8; ++nb) {
-      if constexpr (DX) wf[nb] = wt_frag<T, C::BN>(S + C::XBYTES, 0, 128 * wx + 16 * nb, lane);
-      else wf[nb] = *reinterpret_cast<const F*>(S + wl + nb * 16 * kGRowBytes);
-    }
+    for (int nb = 0; nb < 8; ++nb)
+      wf[nb] = *reinterpret_cast<const F*>(S + wl + nb * 16 * kGRowBytes);
   };
   auto mma_all = [&](const F (&xf)[4], const F (&wf)[8]) {
 #pragma unroll
@@ -295,8 +237,7 @@ __global__ __launch_bounds__(C::THREADS, 512 / C::THREADS) void moe_gemm_kernel(
     char* S = smem + (st % NBUF) * STAGE;
     for (int i = tid; i < (BM + BN) * 4; i += NT) {   // x rows, then W rows (BM is a multiple of 16)
       const int row = i >> 2, pos = i & 3;
-      const bool past = DX && row >= BM ? (i - BM * 4) / C::template wch<T>() >= valid * PER : (pos ^ g_swz(row)) >= valid;
-      if (past) *reinterpret_cast<u32x4*>(S + row * kGRowBytes + pos * 16) = u32x4{0u, 0u, 0u, 0u};
+      if ((pos ^ g_swz(row)) >= valid) *reinterpret_cast<u32x4*>(S + row * kGRowBytes + pos * 16) = u32x4{0u, 0u, 0u, 0u};
     }
     __syncthreads();
   };
@@ -855,14 +796,14 @@ hipError_t launch_moe_stream(MoeArgs a, long P, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, bool DX = false>
+template <typename T>
 hipError_t launch_moe_mid(MoeArgs a, long P, hipStream_t stream) {
   using C = MoeMid;
   a.nt = (a.d_out + C::BN - 1) / C::BN;
   const long max_tiles = ((P + C::BM - 1) / C::BM + a.E) * a.nt;
   const long grid = (max_tiles + kXcds - 1) / kXcds * kXcds;
   if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
-  if (grid > 0) moe_gemm_kernel<T, C, DX><<<(int)grid, C::THREADS, 0, stream>>>(a);
+  if (grid > 0) moe_gemm_kernel<T, C><<<(int)grid, C::THREADS, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -876,6 +817,26 @@ hipError_t launch_moe_large(MoeArgs a, long P, bool wide, hipStream_t stream) {
   else if (wide) moe_gemm_large_kernel<false, true><<<(int)grid, Large::THREADS, 0, stream>>>(a);
   else if (ragged) moe_gemm_large_kernel<true, false><<<(int)grid, Large::THREADS, 0, stream>>>(a);
   else moe_gemm_large_kernel<false, false><<<(int)grid, Large::THREADS, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int NRB, int BN>
+hipError_t launch_moe_dx_stream(MoeArgs a, long P, hipStream_t stream) {
+  using C = DxStream<T, NRB, BN>;
+  a.nt = (a.d_out + C::BN - 1) / C::BN;
+  const long grid = ((P + C::BM - 1) / C::BM + a.E) * a.nt;
+  if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
+  moe_dx_stream_kernel<T, NRB, BN><<<(int)grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_moe_dx_tile(MoeArgs a, long P, hipStream_t stream) {
+  using C = DxTile;
+  a.nt = (a.d_out + C::BN - 1) / C::BN;
+  const long max_tiles = ((P + C::BM - 1) / C::BM + a.E) * a.nt;
+  const long grid = (max_tiles + kXcds - 1) / kXcds * kXcds;
+  if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
+  moe_dx_tile_kernel<<<(int)grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -946,10 +907,61 @@ bool mid_f32(const MoeArgs& a, long P) {
   return 5 * ((tiles + cus - 1) / cus * cus) * BM * BN < 6 * (P + 32 * (long)a.E) * a.d_out;
 }
 
+// The input gradient: which kernel, by the average number of rows per expert
+// (random routings, weights out of every cache, us a call; even routing, then one
+// with popularity ~ 1 / rank^0.8).
+// bf16: streaming with 32 and with 64 rows, large tiles:
+//   contraction 2048, 1024 columns, 64 experts (256 large tiles of one per expert)
+//      8 rows    46 /  48               54 /  51
+//     16 rows    49 /  51               57 /  63
+//     32 rows    69 /  56 /  64         71 /  68 / 108
+//     64 rows   105 /  86 /  70         98 /  79 / 114
+//    128 rows     - / 157 /  73          - / 159 / 115
+//   1024, 2048, 64 (512)
+//     16 rows    50 /  55               53 /  61
+//     24 rows    57 /  58               62 /  64
+//     64 rows   107 /  90 /  76        101 /  84 / 101
+//   14336, 4096, 8 (128)
+//     16 rows   152 / 152              157 / 159
+//     32 rows   268 / 161 / 313        258 / 228 / 310
+//     64 rows   381 / 263 / 312        381 / 284 / 310
+//     96 rows   496 / 328 / 310        490 / 304 / 310
+// (128 columns a block: with 64 the same tiles took 51 to 56 us at 16 rows and 164
+// us at 14336 x 4096; a 16-row form gained 3% at 4 rows and lost from 8 on.)  The
+// large tiles take over at 64 rows, where there are fewer of them than CUs at 96.
+constexpr long kDxStream32 = 20, kDxStream64 = 64, kDxStream64Few = 96;
+// fp32: streaming with 16, 32 and 64 rows (64 columns), tiles:
+//   1024, 512, 8 experts    64 rows     18 /  17 /  24 /  89
+//   2048, 1024, 64           4 rows     92 / 101 / 160 / 297
+//                           16 rows    133 / 105 / 157 / 298
+//                           64 rows    359 / 263 / 267 / 298
+//                          200 rows    865 / 620 / 584 / 572
+//   1024, 2048, 16         128 rows    139 / 115 / 119 / 152
+//                          600 rows    562 / 435 / 392 / 419
+//                         1200 rows   1099 / 836 / 757 / 696
+// From 128 rows on by rounds of tiles: a CU works through its tiles at the rate of
+// its matrix units, 10% faster per element than the streaming kernel, whose small
+// blocks even out.  Both count half a tile lost per expert.
+constexpr long kDxStream16F32 = 8, kDxStream32F32 = 128;
+
+bool dx_tiles_f32(const MoeArgs& a, long P) {
+  const long cus = device_cu_count(), BM = DxTile::BM, BN = DxTile::BN;
+  const long tiles = (P / BM + a.E / 2) * ((a.d_out + BN - 1) / BN);
+  return 9 * ((tiles + cus - 1) / cus * cus) * BM * BN < 10 * (P + 32 * (long)a.E) * a.d_out;
+}
+
 hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream) {
-  if (dtype == ACE_F32) return launch_moe_mid<float, true>(a, P, stream);
-  if (P >= kLargeRows * a.E && a.d_in >= kDxLargeK) return launch_moe_dx_large(a, P, stream);
-  return launch_moe_mid<__bf16, true>(a, P, stream);
+  if (dtype == ACE_F32) {
+    if (P <= kDxStream16F32 * a.E) return launch_moe_dx_stream<float, 1, 64>(a, P, stream);
+    if (P <= kDxStream32F32 * a.E) return launch_moe_dx_stream<float, 2, 64>(a, P, stream);
+    if (dx_tiles_f32(a, P)) return launch_moe_dx_tile(a, P, stream);
+    return launch_moe_dx_stream<float, 4, 64>(a, P, stream);
+  }
+  const bool few = (long)a.E * ((a.d_out + Large::BN - 1) / Large::BN) < device_cu_count();
+  if (P <= kDxStream32 * a.E) return launch_moe_dx_stream<__bf16, 2, 128>(a, P, stream);
+  if (P <= (few ? kDxStream64Few : kDxStream64) * a.E || a.d_in < kDxLargeK)
+    return launch_moe_dx_stream<__bf16, 4, 128>(a, P, stream);
+  return launch_moe_dx_large(a, P, stream);
 }
 
 hipError_t launch_moe_gemm(int dtype, const MoeArgs& a, long P, hipStream_t stream) {
