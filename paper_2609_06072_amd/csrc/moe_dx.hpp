@@ -56,15 +56,24 @@ __device__ inline typename Tr<T>::frag wt_frag(const char* S, int n, int lane) {
   }
 }
 
+// mfma_acc without its wait: for operands that no vector instruction wrote just
+// before (here LDS reads did; the test of these kernels looks for any).  The two
+// wait states of each of 128 instructions a stage were 5% of its time.
+__device__ inline void mfma_ready(f32x4& d, bf16x8 a, bf16x8 b) {
+  asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(d) : "v"(a), "v"(b));
+}
+
 // Four values rounded to bf16, as two words.
 __device__ inline u32x2 round4(f32x4 v) {
   return __builtin_bit_cast(u32x2, bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]});
 }
 
-// RAGGED: K is no multiple of two stages; the chunks past it are zeroed in the
-// fragments (see moe_gemm_large_kernel).  K >= kDxLargeK, so that the copies
-// never run ahead by more than a tile.
+// RAGGED: K is no multiple of two stages; the copies of chunks past it read
+// zeros instead (both operands': an infinity times zero is no zero).  Zeroing the
+// fragments instead cost 0.6 of 1.8 us a stage on the one wave of a SIMD.
+// K >= kDxLargeK, so that the copies never run ahead by more than a tile.
 constexpr int kDxLargeK = 256;
+__device__ const u32x4 kZeros = {0u, 0u, 0u, 0u};
 
 template <bool RAGGED>
 __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs a) {
@@ -168,29 +177,37 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
   int cst = -1;                // stage that this wave copies (x starts half a stage early)
   const char* sbase = base;    // of that stage
   uint32_t colb[2] = {0, 0};   // x: chunk of the lane's column, by copy parity
-  int wgroups = 8;             // W: 8-row groups of the stage inside the contraction
+  // RAGGED: copy i reads zeros where key + i wmul >= K / 8 (x: the chunk; W: the
+  // 8-row group of the stage); one form for both, so that nothing branches
+  uint32_t key[2] = {0, 0};
+  const int wmul = xwave ? 0 : 1;
+  uint64_t zeros = reinterpret_cast<uint64_t>(&kZeros);
+  asm("" : "+s"(zeros));
   // ENDS: the stage may be the first one past the tile (then it is the next
   // tile's first, or the last one again)
   auto begin_copies = [&](int par, bool ends) {
     if (par == (xwave ? 1 : 0)) ++cst;
-    if (ends && cst == nst2) {
-      cst = more ? 0 : nst2 - 1;
-      if (more) set_tile(nxt, pn);
+    if (ends && cst == nst2 && more) {
+      cst = 0;
+      set_tile(nxt, pn);
     }
-    const int st = max(0, min(cst, nst - 1));
+    // (a block without a next tile repeats its last stage)
+    const int st = max(0, min(cst, nst2 - 1));
     if (xwave) {
       sbase = base;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) colb[c] = min(st * (C::KC / 8) + col[c], K / 8 - 1);
+      for (int c = 0; c < 2; ++c) {
+        colb[c] = key[c] = st * (C::KC / 8) + col[c];
+      }
     } else {
       sbase = base + (size_t)st * (C::KC * 2) * N;
-      if (RAGGED) wgroups = min(8, K / 8 - 8 * st);
+      key[0] = key[1] = st * (C::KC / 8);
     }
   };
   auto copy = [&](int par, int i) {
-    // W groups past the contraction repeat its last one
-    const char* b = RAGGED ? sbase + (ptrdiff_t)(min(i, wgroups - 1) - i) * 16 * N : sbase;
-    dma16(b + (size_t)(roff[par][i] + colb[i & 1]) * 16, __builtin_amdgcn_readfirstlane(cslot + i * 1024));
+    uint64_t p = reinterpret_cast<uint64_t>(sbase) + (uint64_t)(roff[par][i] + colb[i & 1]) * 16;
+    if (RAGGED) p = (int)key[i & 1] >= K / 8 - i * wmul ? zeros : p;
+    dma16(reinterpret_cast<const void*>(p), __builtin_amdgcn_readfirstlane(cslot + i * 1024));
   };
   auto end_copies = [&]() {
     cslot += C::SLOT;
@@ -230,14 +247,14 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
       h2[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(smem + rslot + wtl[nb] + (32 * kh + 4 * h) * ROWB));
     return __builtin_bit_cast(F, __builtin_shufflevector(h2[0], h2[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  // Half-step h = PAR of stage st: matrix work on (x0, xc, wc) for the wave's row
+  // Half-step h = PAR of a stage: matrix work on (x0, xc, wc) for the wave's row
   // blocks 4 h .. 4 h + 3; reads the next half's x fragments and half of the next
   // stage's W fragments; copies the slot after next but three.
   // The copies come to the end of the tile in its last stage but two, an odd one.
   // drained: the first four half-steps behind a tile whose 32 stores were all
   // issued.  The slots they read were copied before the stores, which may all be
   // under way.  (Any other order has 24 copies behind the needed ones.)
-  auto half = [&](auto par_c, auto mma_c, auto odd_c, int st, bool drained, F (&x1)[4], F (&wc)[16], F (&x1n)[4], F (&wn)[16]) {
+  auto half = [&](auto par_c, auto mma_c, auto odd_c, bool drained, F (&x1)[4], F (&wc)[16], F (&x1n)[4], F (&wn)[16]) {
     constexpr int PAR = decltype(par_c)::value;
     constexpr bool MMA = decltype(mma_c)::value;
     __builtin_amdgcn_sched_barrier(0);
@@ -250,22 +267,6 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
     const char* xs = smem + rslot + xl;
     const char* xs1 = smem + rslot + (xl ^ 64);
     begin_copies(PAR, decltype(odd_c)::value);
-    const int c = st * C::KC + 8 * g;
-    const bool past = RAGGED && MMA && st * C::KC + C::KC > K;   // wave-uniform
-    if (PAR == 0 && past) {
-#pragma unroll
-      for (int nb = 0; nb < 8; ++nb) {
-        if (c >= K) wc[nb] = Tr<__bf16>::zero();
-        if (c + 32 >= K) wc[nb + 8] = Tr<__bf16>::zero();
-      }
-    }
-    if (past) {
-#pragma unroll
-      for (int mb = 0; mb < 4; ++mb) {
-        if (c >= K) x0[mb] = Tr<__bf16>::zero();
-        if (c + 32 >= K) x1[mb] = Tr<__bf16>::zero();
-      }
-    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (i < 8) {
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
 #pragma unroll
         for (int mb = 0; mb < 4; ++mb) {
           const int nb = i & 7, kh = i >> 3;
-          mfma_acc(acc[nb][4 * PAR + mb], wc[nb + 8 * kh], kh ? x1[mb] : x0[mb]);
+          mfma_ready(acc[nb][4 * PAR + mb], wc[nb + 8 * kh], kh ? x1[mb] : x0[mb]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -291,15 +292,15 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
   using Yes = std::true_type;
   using No = std::false_type;
   __bf16* Y = static_cast<__bf16*>(a.y);
-  half(P0{}, No{}, No{}, 0, false, x1a, wb, x1b, wa);
-  half(P1{}, No{}, No{}, 0, false, x1b, wb, x1a, wa);
+  half(P0{}, No{}, No{}, false, x1a, wb, x1b, wa);
+  half(P1{}, No{}, No{}, false, x1b, wb, x1a, wa);
   bool drained = false;
   for (;;) {
     for (int st = 0; st < nst2; st += 2) {   // two stages: the W fragments change registers
-      half(P0{}, Yes{}, No{}, st, drained, x1a, wa, x1b, wb);
-      half(P1{}, Yes{}, No{}, st, drained, x1b, wa, x1a, wb);
-      half(P0{}, Yes{}, Yes{}, st + 1, drained, x1a, wb, x1b, wa);
-      half(P1{}, Yes{}, Yes{}, st + 1, drained, x1b, wb, x1a, wa);
+      half(P0{}, Yes{}, No{}, drained, x1a, wa, x1b, wb);
+      half(P1{}, Yes{}, No{}, drained, x1b, wa, x1a, wb);
+      half(P0{}, Yes{}, Yes{}, drained, x1a, wb, x1b, wa);
+      half(P1{}, Yes{}, Yes{}, drained, x1b, wb, x1a, wa);
       drained = false;
     }
     // ---- the tile after next, then this tile's results: lane (c16, g) holds
@@ -369,21 +370,21 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
 // LDS at the end, in wave order.  A third buffer per wave gained nothing (fewer
 // streams at a time serve HBM better).  64 experts of 2048 x 1024 with 4 rows
 // each: 44 us, 5.9 TB/s of weights.
-template <typename T, int NRB, int BN_>
+template <typename T, int NRB, int BN_, int NW_ = 4, int NBUF_ = 2>
 struct DxStream {
-  static constexpr int KB = Tr<T>::KB, BM = 16 * NRB, BN = BN_, NBUF = 2, NCB = BN / 16;
+  static constexpr int KB = Tr<T>::KB, BM = 16 * NRB, BN = BN_, NW = NW_, NBUF = NBUF_, NCB = BN / 16;
   static constexpr int WBYTES = KB * BN * (int)sizeof(T), STAGE = WBYTES + BM * kGRowBytes;
   static constexpr int NS = WBYTES / 1024;                  // W copies of a stage
   static constexpr int WCH = BN * (int)sizeof(T) / 16;      // chunks of a W row
   static constexpr int CST = BN + 4;                        // row stride of the sums
-  static constexpr int RING = 4 * NBUF * STAGE, SUMS = 4 * BM * CST * 4;
+  static constexpr int RING = NW * NBUF * STAGE, SUMS = NW * BM * CST * 4;
 };
 
-template <typename T, int NRB, int BN>
-__global__ __launch_bounds__(256) void moe_dx_stream_kernel(MoeArgs a) {
-  using C = DxStream<T, NRB, BN>;
+template <typename T, int NRB, int BN, int NW, int NBUF>
+__global__ __launch_bounds__(64 * NW) void moe_dx_stream_kernel(MoeArgs a) {
+  using C = DxStream<T, NRB, BN, NW, NBUF>;
   using F = typename Tr<T>::frag;
-  constexpr int PER = Tr<T>::PER, KB = C::KB, NCB = C::NCB, NBUF = C::NBUF;
+  constexpr int PER = Tr<T>::PER, KB = C::KB, NCB = C::NCB;
   __shared__ __attribute__((aligned(16))) char smem[C::RING > C::SUMS ? C::RING : C::SUMS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, g = lane >> 4;
@@ -407,10 +408,10 @@ __global__ __launch_bounds__(256) void moe_dx_stream_kernel(MoeArgs a) {
   constexpr int RPC = 64 / C::WCH;
   auto col_of = [&](int i) { return min(PER * ((lane % C::WCH) ^ wt_swz<T, BN>(RPC * i + wrow)), N - PER - n0); };
   const int nst = (K + KB - 1) / KB;
-  const int mine = (nst - wave + 3) / 4;    // K-blocks of this wave
+  const int mine = (nst - wave + NW - 1) / NW;    // K-blocks of this wave
   char* ring = smem + wave * NBUF * C::STAGE;
   auto issue = [&](int i) {
-    const int k0 = (wave + 4 * i) * KB;
+    const int k0 = (wave + NW * i) * KB;
     const uint32_t buf = lds_addr(ring) + (i % NBUF) * C::STAGE;
     const T* Wk = Wt + (size_t)k0 * N;
 #pragma unroll
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(256) void moe_dx_stream_kernel(MoeArgs a) {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     const char* S = ring + (i % NBUF) * C::STAGE;
-    const bool past = (wave + 4 * i) * KB + PER * g >= K;
+    const bool past = (wave + NW * i) * KB + PER * g >= K;
     F wf[NCB], xf[NRB];
 #pragma unroll
     for (int nb = 0; nb < NCB; ++nb) {
@@ -470,11 +471,11 @@ __global__ __launch_bounds__(256) void moe_dx_stream_kernel(MoeArgs a) {
   typedef __attribute__((ext_vector_type(4))) T T4;
   T* Y = static_cast<T*>(a.y);
 #pragma unroll
-  for (int i = 0; i < NRB * BN / 64; ++i) {
-    const int it = 256 * i + threadIdx.x, row = it / (BN / 4), col = 4 * (it % (BN / 4));
+  for (int i = 0; i < NRB * BN / (16 * NW); ++i) {
+    const int it = 64 * NW * i + threadIdx.x, row = it / (BN / 4), col = 4 * (it % (BN / 4));
     f32x4 v = *reinterpret_cast<const f32x4*>(sums + row * C::CST + col);
 #pragma unroll
-    for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * C::BM + row) * C::CST + col);
+    for (int w = 1; w < NW; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * C::BM + row) * C::CST + col);
     if (u0 + row < u_end && n0 + col < N)
       *reinterpret_cast<T4*>(Y + (size_t)a.pair_list[u0 + row] * N + n0 + col) = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
   }

@@ -820,13 +820,13 @@ hipError_t launch_moe_large(MoeArgs a, long P, bool wide, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, int NRB, int BN>
+template <typename T, int NRB, int BN, int NW = 4, int NBUF = 2>
 hipError_t launch_moe_dx_stream(MoeArgs a, long P, hipStream_t stream) {
-  using C = DxStream<T, NRB, BN>;
+  using C = DxStream<T, NRB, BN, NW, NBUF>;
   a.nt = (a.d_out + C::BN - 1) / C::BN;
   const long grid = ((P + C::BM - 1) / C::BM + a.E) * a.nt;
   if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
-  moe_dx_stream_kernel<T, NRB, BN><<<(int)grid, 256, 0, stream>>>(a);
+  moe_dx_stream_kernel<T, NRB, BN, NW, NBUF><<<(int)grid, 64 * NW, 0, stream>>>(a);
   return hipGetLastError();
 }
 
