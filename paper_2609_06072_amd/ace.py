@@ -524,6 +524,11 @@ def _check_routing(routing: Routing, T: int, k: int, device) -> None:
         raise ValueError(f"routing is on {routing.pair_row.device}, expected {device}")
 
 
+# a per-pair input gradient without a workspace computes the same sums in one piece;
+# small calls are given one
+_DX_SPLIT_ELEMS = 1 << 19
+
+
 def ace_moe_dx(dy, W, expert_routing: Routing, dx=None, input_mode: int = ACE_INPUT_SHARED,
                accumulate: bool = False, ws=None, stream=None) -> torch.Tensor:
     """Input gradient of the frozen expert projection (include/ace.h): per pair
@@ -545,7 +550,7 @@ def ace_moe_dx(dy, W, expert_routing: Routing, dx=None, input_mode: int = ACE_IN
         dx = _alloc(torch.empty if shared else torch.zeros, stream, rows, d_in, dtype=W.dtype,
                     device=device)
     _want("dx", dx, rows * d_in, W.dtype, device)
-    if ws is None and (shared or accumulate):
+    if ws is None and (shared or accumulate or T * k * d_in <= _DX_SPLIT_ELEMS):
         need = ace_workspace_bytes(ACE_OP_MOE_DX, T, k, d_in, d_out, E, 0)
         ws = _alloc(torch.empty, stream, max(need, 256), dtype=torch.uint8, device=device)
     _want("ws", ws, None, torch.uint8, device, optional=True)

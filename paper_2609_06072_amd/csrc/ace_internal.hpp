@@ -113,6 +113,9 @@ struct MoeArgs {
   const int32_t* row_token;
   const uint32_t* row_slots;
   const int32_t* pair_list;   // launch_moe_dx: pair of each row
+  float* part;                // launch_moe_dx: sums of the splits
+  long pairs;
+  int32_t splits;
   int32_t E, k, d_in, d_out, per_pair;
   const void* H;              // [U'][rpad] scaled shrink per adapter row, or null (no adapter)
   int32_t rpad;
@@ -128,6 +131,23 @@ hipError_t launch_moe_gemm(int dtype, const MoeArgs& a, long P, hipStream_t stre
 // the output's gradient [T*k][d_in], W [E][d_in][d_out] (d_in, d_out: the
 // product's own contraction length and columns), per_pair, no adapter.
 hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream);
+// Blocks that share a tile of that product (1: a.y is written; otherwise a.part,
+// [splits][P][d_out] fp32, to be joined).  At most kDxMaxSplits, and 1 where P *
+// d_out passes kDxSplitElems.
+constexpr int kDxMaxSplits = 8;
+constexpr long kDxSplitElems = 1L << 19;
+int moe_dx_splits(int dtype, const MoeArgs& a, long P);
+struct DxJoinArgs {
+  const float* part;          // [splits][pairs][d]
+  const int32_t* pair_row;
+  void* out;                  // [pairs / k][d]
+  long pairs;
+  int32_t splits, k, d, accumulate;
+  int32_t keep;               // k == 1: rows of dropped pairs are left alone
+  FastDiv per_row;            // (set by the launcher)
+  uint32_t pieces;
+};
+hipError_t launch_moe_dx_join(int dtype, DxJoinArgs a, hipStream_t stream);
 
 // Weighted sum of a token's expert outputs, and its gradient (combine.hip).
 struct CombineArgs {

@@ -296,7 +296,10 @@ ace_status check_rows(ace_dtype dtype, int32_t d) {
 // to below 2^31 with a block to spare.
 constexpr int64_t kMaxRowElems = ((int64_t)1 << 33) - 4096;
 
-size_t moe_dx_ws_bytes(int T, int k, int d_in) { return (size_t)T * k * d_in * sizeof(float); }
+size_t moe_dx_ws_bytes(int T, int k, int d_in) {
+  const size_t rows = (size_t)T * k * d_in;
+  return rows * (rows <= (size_t)kDxSplitElems ? kDxMaxSplits : 1) * sizeof(float);
+}
 
 ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, int32_t d_in,
                       int32_t d_out, int32_t E, const void* dy, const void* W,
@@ -331,7 +334,7 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   if (!aligned(dy, 16) || !aligned(W, 16) || !aligned(dx, 16))
     return fail(ACE_ERR_INVALID_ARG, "dy, W and dx must be 16-byte aligned");
   const bool pair_rows = im == ACE_INPUT_SHARED || accumulate;
-  if (pair_rows) {
+  if (pair_rows || ws) {
     const size_t need = moe_dx_ws_bytes(T, k, d_in);
     if (need > 0 && (!ws || ws_bytes < need))
       return fail(ACE_ERR_WORKSPACE, "the input gradient needs %zu workspace bytes, got %zu", need,
@@ -353,7 +356,24 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   a.d_out = d_in;
   a.per_pair = 1;
   a.y = pair_rows ? ws : dx;
-  hipError_t e = launch_moe_dx(dtype, a, (long)T * k, st);
+  const long P = (long)T * k;
+  a.pairs = P;
+  a.splits = ws ? moe_dx_splits(dtype, a, P) : 1;
+  a.part = static_cast<float*>(ws);
+  hipError_t e = launch_moe_dx(dtype, a, P, st);
+  if (e == hipSuccess && a.splits > 1) {
+    DxJoinArgs j{};
+    j.part = a.part;
+    j.pair_row = ert->pair_row;
+    j.out = dx;
+    j.pairs = P;
+    j.splits = a.splits;
+    j.k = im == ACE_INPUT_SHARED ? k : 1;
+    j.d = d_in;
+    j.accumulate = accumulate;
+    j.keep = im == ACE_INPUT_PER_PAIR;
+    return hip_status(launch_moe_dx_join(dtype, j, st), "input gradient join launch");
+  }
   if (e != hipSuccess || !pair_rows) return hip_status(e, "input gradient launch");
   // the token's rows, or (per pair) each row as a token of its own
   CombineArgs c{};

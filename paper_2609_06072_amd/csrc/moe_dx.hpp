@@ -363,32 +363,35 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
 
 // ---- few rows per expert: the weights bound the call, and a block streams them.
 //
-// A block takes up to 16 NRB rows of one expert and BN columns (256 bytes of a W
-// row).  Its four waves split the contraction: wave w takes the K-blocks w, w +
+// A block takes up to 16 NRB rows of one expert and BN columns (128 to 256 bytes
+// of a W row).  Its four waves split the contraction: wave w takes the K-blocks w, w +
 // 4, ..., each through a ring of its own in LDS (the K-block's W rows and the same
 // columns of the x rows), so no barrier stands in the loop; the four sums meet in
-// LDS at the end, in wave order.  A third buffer per wave gained nothing (fewer
+// LDS at the end, in wave order.  Where even the smallest tiles leave CUs idle,
+// several blocks share a tile's K-blocks in the same way (a.splits) and write fp32
+// sums that moe_dx_join_kernel adds, in order.  A third buffer per wave gained nothing (fewer
 // streams at a time serve HBM better).  64 experts of 2048 x 1024 with 4 rows
 // each: 44 us, 5.9 TB/s of weights.
-template <typename T, int NRB, int BN_, int NW_ = 4, int NBUF_ = 2>
+template <typename T, int NRB, int BN_>
 struct DxStream {
-  static constexpr int KB = Tr<T>::KB, BM = 16 * NRB, BN = BN_, NW = NW_, NBUF = NBUF_, NCB = BN / 16;
+  static constexpr int KB = Tr<T>::KB, BM = 16 * NRB, BN = BN_, NBUF = 2, NCB = BN / 16;
   static constexpr int WBYTES = KB * BN * (int)sizeof(T), STAGE = WBYTES + BM * kGRowBytes;
   static constexpr int NS = WBYTES / 1024;                  // W copies of a stage
   static constexpr int WCH = BN * (int)sizeof(T) / 16;      // chunks of a W row
   static constexpr int CST = BN + 4;                        // row stride of the sums
-  static constexpr int RING = NW * NBUF * STAGE, SUMS = NW * BM * CST * 4;
+  static constexpr int RING = 4 * NBUF * STAGE, SUMS = 4 * BM * CST * 4;
 };
 
-template <typename T, int NRB, int BN, int NW, int NBUF>
-__global__ __launch_bounds__(64 * NW) void moe_dx_stream_kernel(MoeArgs a) {
-  using C = DxStream<T, NRB, BN, NW, NBUF>;
+template <typename T, int NRB, int BN>
+__global__ __launch_bounds__(256) void moe_dx_stream_kernel(MoeArgs a) {
+  using C = DxStream<T, NRB, BN>;
   using F = typename Tr<T>::frag;
-  constexpr int PER = Tr<T>::PER, KB = C::KB, NCB = C::NCB;
+  constexpr int PER = Tr<T>::PER, KB = C::KB, NCB = C::NCB, NBUF = C::NBUF;
   __shared__ __attribute__((aligned(16))) char smem[C::RING > C::SUMS ? C::RING : C::SUMS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, g = lane >> 4;
-  const int mt = blockIdx.x / a.nt, n0 = (blockIdx.x % a.nt) * C::BN;
+  const int tile = blockIdx.x / a.splits;
+  const int mt = tile / a.nt, n0 = (tile % a.nt) * C::BN;
   int e, u0, u_end;
   if (!locate_tile(a.offsets, a.E, C::BM, mt, &e, &u0, &u_end)) return;   // block-uniform
   e = __builtin_amdgcn_readfirstlane(e);
@@ -408,10 +411,12 @@ __global__ __launch_bounds__(64 * NW) void moe_dx_stream_kernel(MoeArgs a) {
   constexpr int RPC = 64 / C::WCH;
   auto col_of = [&](int i) { return min(PER * ((lane % C::WCH) ^ wt_swz<T, BN>(RPC * i + wrow)), N - PER - n0); };
   const int nst = (K + KB - 1) / KB;
-  const int mine = (nst - wave + NW - 1) / NW;    // K-blocks of this wave
+  // K-blocks of this wave: first, first + stride, ...
+  const int stride = 4 * a.splits, first = 4 * (blockIdx.x % a.splits) + wave;
+  const int mine = max(0, (nst - first + stride - 1) / stride);
   char* ring = smem + wave * NBUF * C::STAGE;
   auto issue = [&](int i) {
-    const int k0 = (wave + NW * i) * KB;
+    const int k0 = (first + stride * i) * KB;
     const uint32_t buf = lds_addr(ring) + (i % NBUF) * C::STAGE;
     const T* Wk = Wt + (size_t)k0 * N;
 #pragma unroll
@@ -442,7 +447,7 @@ __global__ __launch_bounds__(64 * NW) void moe_dx_stream_kernel(MoeArgs a) {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     const char* S = ring + (i % NBUF) * C::STAGE;
-    const bool past = (wave + NW * i) * KB + PER * g >= K;
+    const bool past = (first + stride * i) * KB + PER * g >= K;
     F wf[NCB], xf[NRB];
 #pragma unroll
     for (int nb = 0; nb < NCB; ++nb) {
@@ -471,14 +476,42 @@ __global__ __launch_bounds__(64 * NW) void moe_dx_stream_kernel(MoeArgs a) {
   typedef __attribute__((ext_vector_type(4))) T T4;
   T* Y = static_cast<T*>(a.y);
 #pragma unroll
-  for (int i = 0; i < NRB * BN / (16 * NW); ++i) {
-    const int it = 64 * NW * i + threadIdx.x, row = it / (BN / 4), col = 4 * (it % (BN / 4));
+  for (int i = 0; i < NRB * BN / 64; ++i) {
+    const int it = 256 * i + threadIdx.x, row = it / (BN / 4), col = 4 * (it % (BN / 4));
     f32x4 v = *reinterpret_cast<const f32x4*>(sums + row * C::CST + col);
 #pragma unroll
-    for (int w = 1; w < NW; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * C::BM + row) * C::CST + col);
-    if (u0 + row < u_end && n0 + col < N)
-      *reinterpret_cast<T4*>(Y + (size_t)a.pair_list[u0 + row] * N + n0 + col) = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * C::BM + row) * C::CST + col);
+    if (u0 + row < u_end && n0 + col < N) {
+      const size_t at = (size_t)a.pair_list[u0 + row] * N + n0 + col;
+      if (a.splits > 1) *reinterpret_cast<f32x4*>(a.part + (size_t)(blockIdx.x % a.splits) * a.pairs * N + at) = v;
+      else *reinterpret_cast<T4*>(Y + at) = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    }
   }
+}
+
+// dx (four columns per thread) from the sums of the splits: of one pair, or of a
+// token's routed slots in slot order.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
+  typedef __attribute__((ext_vector_type(4))) T T4;
+  const uint32_t idx = blockIdx.x * kThreads + threadIdx.x;
+  if (idx >= a.pieces) return;
+  const uint32_t t = a.per_row.div(idx), col = 4 * (idx - t * a.per_row.d);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < a.k; ++j) {
+    const size_t p = (size_t)t * a.k + j;
+    if (a.pair_row[p] < 0) {
+      if (a.k == 1 && a.keep) return;   // a dropped pair's own row is left alone
+      continue;
+    }
+    for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(a.part + ((size_t)s * a.pairs + p) * a.d + col);
+  }
+  T4* out = reinterpret_cast<T4*>(static_cast<T*>(a.out) + (size_t)t * a.d + col);
+  if (a.accumulate) {
+    const T4 o = *out;
+    v += f32x4{(float)o[0], (float)o[1], (float)o[2], (float)o[3]};
+  }
+  *out = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
 }
 
 // ---- fp32, many rows per expert: tiles of 128 rows x 128 columns, four waves of

@@ -26,6 +26,7 @@
 // round-robin; block b takes tile (b % 8) * ceil(n_tiles / 8) + b / 8, so each
 // XCD walks a contiguous run of tiles (expert-major): an expert's weight
 // slices stay in one L2.
+#include <algorithm>
 #include <type_traits>
 
 #include "ace_device.hpp"
@@ -820,13 +821,13 @@ hipError_t launch_moe_large(MoeArgs a, long P, bool wide, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, int NRB, int BN, int NW = 4, int NBUF = 2>
+template <typename T, int NRB, int BN>
 hipError_t launch_moe_dx_stream(MoeArgs a, long P, hipStream_t stream) {
-  using C = DxStream<T, NRB, BN, NW, NBUF>;
+  using C = DxStream<T, NRB, BN>;
   a.nt = (a.d_out + C::BN - 1) / C::BN;
-  const long grid = ((P + C::BM - 1) / C::BM + a.E) * a.nt;
+  const long grid = ((P + C::BM - 1) / C::BM + a.E) * a.nt * a.splits;
   if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
-  moe_dx_stream_kernel<T, NRB, BN, NW, NBUF><<<(int)grid, 64 * NW, 0, stream>>>(a);
+  moe_dx_stream_kernel<T, NRB, BN><<<(int)grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -907,61 +908,118 @@ bool mid_f32(const MoeArgs& a, long P) {
   return 5 * ((tiles + cus - 1) / cus * cus) * BM * BN < 6 * (P + 32 * (long)a.E) * a.d_out;
 }
 
-// The input gradient: which kernel, by the average number of rows per expert
-// (random routings, weights out of every cache, us a call; even routing, then one
-// with popularity ~ 1 / rank^0.8).
-// bf16: streaming with 32 and with 64 rows, large tiles:
-//   contraction 2048, 1024 columns, 64 experts (256 large tiles of one per expert)
-//      8 rows    46 /  48               54 /  51
-//     16 rows    49 /  51               57 /  63
-//     32 rows    69 /  56 /  64         71 /  68 / 108
-//     64 rows   105 /  86 /  70         98 /  79 / 114
-//    128 rows     - / 157 /  73          - / 159 / 115
-//   1024, 2048, 64 (512)
-//     16 rows    50 /  55               53 /  61
-//     24 rows    57 /  58               62 /  64
-//     64 rows   107 /  90 /  76        101 /  84 / 101
-//   14336, 4096, 8 (128)
-//     16 rows   152 / 152              157 / 159
-//     32 rows   268 / 161 / 313        258 / 228 / 310
-//     64 rows   381 / 263 / 312        381 / 284 / 310
-//     96 rows   496 / 328 / 310        490 / 304 / 310
-// (128 columns a block: with 64 the same tiles took 51 to 56 us at 16 rows and 164
-// us at 14336 x 4096; a 16-row form gained 3% at 4 rows and lost from 8 on.)  The
-// large tiles take over at 64 rows, where there are fewer of them than CUs at 96.
-constexpr long kDxStream32 = 20, kDxStream64 = 64, kDxStream64Few = 96;
-// fp32: streaming with 16, 32 and 64 rows (64 columns), tiles:
-//   1024, 512, 8 experts    64 rows     18 /  17 /  24 /  89
-//   2048, 1024, 64           4 rows     92 / 101 / 160 / 297
-//                           16 rows    133 / 105 / 157 / 298
-//                           64 rows    359 / 263 / 267 / 298
-//                          200 rows    865 / 620 / 584 / 572
-//   1024, 2048, 16         128 rows    139 / 115 / 119 / 152
-//                          600 rows    562 / 435 / 392 / 419
-//                         1200 rows   1099 / 836 / 757 / 696
+namespace {
+
+// The input gradient: which kernel.  The number of tiles of bm x bn is estimated
+// from the average number of rows per expert (half a tile lost in each; the host
+// does not know the routing), one for every expert that can be hit at least.
+enum DxKernel { kDxS16x64, kDxS32x64, kDxS64x64, kDxS32x128, kDxS64x128, kDxTiles, kDxLarge };
+
+long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
+  const long hit = P < a.E ? P : a.E, rows = P / bm + a.E / 2;
+  return (rows > hit ? rows : hit) * ((a.d_out + bn - 1) / bn);
+}
+
+// bf16.  Two estimates, of rounds of blocks over the CUs (K the contraction):
+//   large tiles  a round of 8 us + 24 us per 1000 of K (20 where no stage is ragged)
+//   streaming, 64 rows x 128 columns (one block per CU)   4 us + 9.5 us per 1000
+// decide between the two (us a call, measured 64 x 128 / large, random routings,
+// weights out of every cache):
+//   K, columns, experts     rows per expert
+//   2048, 1024, 64           32    56 /  64        64    87 /  68      100   117 /  71
+//   4096, 4096, 8            64    88 /  94       128   128 /  93
+//   14336, 4096, 8           64   263 / 312       128   543 / 343
+//   1000, 2056, 16           64    35 /  40       128    65 /  43
+//   304, 3232, 16            20    15 /  20       100    31 /  22
+//   616, 336, 32            200    26 /  26       600    54 /  29
+//   5032, 456, 16           444   138 / 141      1000   282 / 145
+//   1568, 424, 4            981    23 /  49      2000    42 /  50
+//   512, 256, 8            1000    10 /  20      4000    35 /  22
+// Among the streaming forms (32 x 64 / 64 x 64 / 32 x 128 / 64 x 128), the first
+// that fits the chip once (CUs; 1.25 CUs for 64 x 64, of which two share one), and
+// 128 columns beyond:
+//   1568, 424, 4             20    13 /  13 /  17 /  18     300    26 /  19 /  17 /  21
+//   8944, 792, 8             20    64 /  64 /  82 /  83     100   160 /  92 / 112 / 115
+//   1024, 1024, 16           16     9 /  10 /  11 /  12      64    18 /  17 /  18 /  15
+//   2048, 1024, 64           16    55 /  55 /  49 /  51      32     - /   - /  69 /  56
+//   14336, 4096, 8           16     - / 164 / 152 / 152      32     - / 190 / 268 / 161
+constexpr long kDxStream32 = 20;
+
+DxKernel dx_kernel_bf16(const MoeArgs& a, long P) {
+  const long cus = device_cu_count(), K = a.d_in;
+  auto rounds = [&](long blocks) { return (blocks + cus - 1) / cus; };
+  const long large = rounds(dx_blocks(a, P, Large::BM, Large::BN)) * (8000 + (K % (2 * Large::KC) ? 24 : 20) * K);
+  const long stream = rounds(dx_blocks(a, P, 64, 128)) * (8000 + 19 * K) / 2;
+  if (K >= kDxLargeK && P > kDxStream32 * a.E && large < stream) return kDxLarge;
+  if (dx_blocks(a, P, 32, 64) <= cus) return kDxS32x64;
+  if (4 * dx_blocks(a, P, 64, 64) <= 5 * cus) return kDxS64x64;
+  return P <= kDxStream32 * a.E ? kDxS32x128 : kDxS64x128;
+}
+
+// fp32: streaming with 16, 32 and 64 rows (64 columns), tiles, us a call:
+//   1024, 512, 8            64    18 /  17 /  24 /  89
+//   2048, 1024, 64           4    92 / 101 / 160 / 297      16   133 / 105 / 157 / 298
+//                           64   359 / 263 / 267 / 298     200   865 / 620 / 584 / 572
+//   1024, 2048, 16         128   139 / 115 / 119 / 152     600   562 / 435 / 392 / 419
+//                         1200  1099 / 836 / 757 / 696
 // From 128 rows on by rounds of tiles: a CU works through its tiles at the rate of
 // its matrix units, 10% faster per element than the streaming kernel, whose small
 // blocks even out.  Both count half a tile lost per expert.
 constexpr long kDxStream16F32 = 8, kDxStream32F32 = 128;
 
-bool dx_tiles_f32(const MoeArgs& a, long P) {
+DxKernel dx_kernel_f32(const MoeArgs& a, long P) {
+  if (P <= kDxStream16F32 * a.E) return kDxS16x64;
+  if (P <= kDxStream32F32 * a.E) return kDxS32x64;
   const long cus = device_cu_count(), BM = DxTile::BM, BN = DxTile::BN;
   const long tiles = (P / BM + a.E / 2) * ((a.d_out + BN - 1) / BN);
-  return 9 * ((tiles + cus - 1) / cus * cus) * BM * BN < 10 * (P + 32 * (long)a.E) * a.d_out;
+  const bool ahead = 9 * ((tiles + cus - 1) / cus * cus) * BM * BN < 10 * (P + 32 * (long)a.E) * a.d_out;
+  return ahead ? kDxTiles : kDxS64x64;
+}
+
+DxKernel dx_kernel(int dtype, const MoeArgs& a, long P) {
+  return dtype == ACE_F32 ? dx_kernel_f32(a, P) : dx_kernel_bf16(a, P);
+}
+
+}  // namespace
+
+// A block of the narrow forms takes 4 us per 1000 of the contraction, 31 GB/s of
+// weights on its CU; the join costs 3 us more.  (9816 x 544, 4 experts, 1 row each:
+// 43 us in one.)
+int moe_dx_splits(int dtype, const MoeArgs& a, long P) {
+  if (P * a.d_out > kDxSplitElems) return 1;
+  long bm;
+  switch (dx_kernel(dtype, a, P)) {
+    case kDxS16x64: bm = 16; break;
+    case kDxS32x64: bm = 32; break;
+    case kDxS64x64: bm = 64; break;
+    default: return 1;
+  }
+  const long s = device_cu_count() / dx_blocks(a, P, bm, 64), most = a.d_in / 1024;
+  return (int)std::max(1L, std::min({s, most, (long)kDxMaxSplits}));
 }
 
 hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream) {
+  const DxKernel k = dx_kernel(dtype, a, P);
   if (dtype == ACE_F32) {
-    if (P <= kDxStream16F32 * a.E) return launch_moe_dx_stream<float, 1, 64>(a, P, stream);
-    if (P <= kDxStream32F32 * a.E) return launch_moe_dx_stream<float, 2, 64>(a, P, stream);
-    if (dx_tiles_f32(a, P)) return launch_moe_dx_tile(a, P, stream);
-    return launch_moe_dx_stream<float, 4, 64>(a, P, stream);
+    if (k == kDxS16x64) return launch_moe_dx_stream<float, 1, 64>(a, P, stream);
+    if (k == kDxS32x64) return launch_moe_dx_stream<float, 2, 64>(a, P, stream);
+    if (k == kDxS64x64) return launch_moe_dx_stream<float, 4, 64>(a, P, stream);
+    return launch_moe_dx_tile(a, P, stream);
   }
-  const bool few = (long)a.E * ((a.d_out + Large::BN - 1) / Large::BN) < device_cu_count();
-  if (P <= kDxStream32 * a.E) return launch_moe_dx_stream<__bf16, 2, 128>(a, P, stream);
-  if (P <= (few ? kDxStream64Few : kDxStream64) * a.E || a.d_in < kDxLargeK)
-    return launch_moe_dx_stream<__bf16, 4, 128>(a, P, stream);
+  if (k == kDxS32x64) return launch_moe_dx_stream<__bf16, 2, 64>(a, P, stream);
+  if (k == kDxS64x64) return launch_moe_dx_stream<__bf16, 4, 64>(a, P, stream);
+  if (k == kDxS32x128) return launch_moe_dx_stream<__bf16, 2, 128>(a, P, stream);
+  if (k == kDxS64x128) return launch_moe_dx_stream<__bf16, 4, 128>(a, P, stream);
   return launch_moe_dx_large(a, P, stream);
+}
+
+hipError_t launch_moe_dx_join(int dtype, DxJoinArgs a, hipStream_t stream) {
+  a.per_row = FastDiv(a.d / 4);
+  a.pieces = (uint32_t)(a.pairs / a.k * (a.d / 4));
+  const unsigned grid = (a.pieces + kThreads - 1) / kThreads;
+  if (dtype == ACE_BF16) moe_dx_join_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a);
+  else moe_dx_join_kernel<float><<<grid, kThreads, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_moe_gemm(int dtype, const MoeArgs& a, long P, hipStream_t stream) {

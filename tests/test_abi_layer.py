@@ -41,7 +41,7 @@ INV, UNS, WSP = -1, -2, -3
     (dict(dy=None), INV), (dict(W=None), INV), (dict(dx=None), INV),
     (dict(dy=P(0x1008)), INV), (dict(W=P(0x1004)), INV), (dict(dx=P(0x1002)), INV),
     (dict(ws=None), WSP), (dict(wsb=255), WSP), (dict(ws=P(0x100010)), WSP),
-    (dict(im=1, acc=1, ws=None), WSP),
+    (dict(im=1, acc=1, ws=None), WSP), (dict(im=1, wsb=255), WSP), (dict(im=1, ws=P(0x100010)), WSP),
 ])
 def test_moe_dx_refusals(ace, no_device, change, want):
     T, k, E = 4, 2, 4
@@ -69,7 +69,8 @@ def test_empty_calls_do_nothing(ace, no_device):
 
 def test_workspace_query(ace):
     n = ace.ace_workspace_bytes(ace.ACE_OP_MOE_DX, 100, 3, 40, 64, 5, 0)
-    assert n % 256 == 0 and n >= 100 * 3 * 40 * 4
+    assert n % 256 == 0 and n >= 8 * 100 * 3 * 40 * 4
+    assert ace.ace_workspace_bytes(ace.ACE_OP_MOE_DX, 100000, 3, 40, 64, 5, 0) < 2 * 100000 * 3 * 40 * 4
     assert ace.ace_workspace_bytes(ace.ACE_OP_MOE_DX, 0, 3, 40, 64, 5, 0) == 0
     for bad in (dict(d_in=0), dict(T=1 << 30)):
         a = dict(T=100, k=3, d_in=40)

@@ -99,6 +99,10 @@ DX_SIZES = [
     (2100, 1, 2, 264, 136, 0.02, 0.0),
     (257, 32, 40, 64, 48, 0.3, 0.0),        # the most slots
     (90, 2, 256, 64, 64, 0.0, 0.0),         # the most experts
+    (2, 2, 8, 544, 4104, 0.0, 0.0),         # few tiles: several blocks a contraction
+    (40, 3, 4, 72, 2056, 0.2, 0.0),
+    (1300, 2, 8, 264, 328, 0.02, 0.8),      # a ragged contraction in large tiles
+    (700, 2, 2, 1096, 384, 0.0, 0.0),
 ]
 
 
@@ -159,6 +163,25 @@ def test_moe_dx_infinities_stay_in_their_rows(ace, dtype):
         ref, tol = dx_refs(f64(torch.nan_to_num(dy, posinf=0)), f64(torch.nan_to_num(W, posinf=0)), ids, E, dtype, False)
         keep = clean.cpu().numpy()
         close("finite rows", f64(dx)[keep], ref[keep], tol[keep])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_moe_dx_without_a_workspace(ace, dtype):
+    """Per pair the workspace is optional; with it, a long contraction in few
+    tiles is shared, and the sums differ in their last bits at most."""
+    T, k, E, d_in, d_out = 3, 2, 4, 72, 9000
+    ids = draw_ids(T, k, E, 18)
+    rt = route(ace, ids, E)
+    dy, W = gen(19, T * k, d_out, dtype=dtype), gen(20, E, d_out, d_in, dtype=dtype)
+    ref, tol = dx_refs(f64(dy), f64(W), ids, E, dtype, False)
+    dx = torch.full((T * k, d_in), 7.0, dtype=DT[dtype], device="cuda")
+    import ctypes
+    st = ace.raw_lib().ace_moe_dx(int(dtype == "bf16"), 1, T, k, d_in, d_out, E, dy.data_ptr(), W.data_ptr(),
+                                  ctypes.byref(rt.c), 0, dx.data_ptr(), None, 0,
+                                  torch.cuda.current_stream().cuda_stream or None)
+    assert st == 0, ace.ace_last_error()
+    close("without", dx, ref, tol)
+    close("with", ace.ace_moe_dx(dy, W, rt, input_mode=ace.ACE_INPUT_PER_PAIR), ref, tol)
 
 
 def test_moe_dx_all_dropped_and_repeated(ace):
