@@ -499,12 +499,43 @@ def ace_moe_lora_fwd(x, W, expert_routing: Routing, y, key_rank: Optional[Sequen
            "ace_moe_lora_fwd")
 
 
-def _on_device(t: torch.Tensor) -> torch.device:
-    """The device of a call's first tensor, which must be the current one: the
-    library launches on the current device's stream."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+# The calls below check each tensor in one function (a call of a few microseconds
+# is bound by the host), and refuse tensors of another device than the current one:
+# the library launches on the current device's stream.
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on_device(t: torch.Tensor) -> int:
+    """Index of the tensor's device, which must be the current one."""
+    index = t.get_device()
+    if index < 0 or index != _get_device():
         raise ValueError(f"tensors are on {t.device}, which is not the current GPU")
-    return t.device
+    return index
+
+
+def _arg(name: str, t, numel: int, dtype, index: int) -> Optional[int]:
+    """Pointer of a tensor argument of the given size, type and device."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to libace must be contiguous")
+    return t.data_ptr() or None
+
+
+def _opt(name: str, t, numel: int, dtype, index: int) -> Optional[int]:
+    return None if t is None else _arg(name, t, numel, dtype, index)
+
+
+def _stream_on(index: int, stream) -> Optional[int]:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(index) or None
+    return _stream(stream)
 
 
 def _alloc(make, stream, *shape, **kw):
@@ -516,12 +547,12 @@ def _alloc(make, stream, *shape, **kw):
         return make(*shape, **kw)
 
 
-def _check_routing(routing: Routing, T: int, k: int, device) -> None:
+def _check_routing(routing: Routing, T: int, k: int, index: int) -> None:
     if (routing.c.T, routing.c.k) != (T, k):
         raise ValueError(f"routing was built for T={routing.c.T} k={routing.c.k}, the call has "
                          f"T={T} k={k}")
-    if routing.pair_row.device != device:
-        raise ValueError(f"routing is on {routing.pair_row.device}, expected {device}")
+    if routing.pair_row.get_device() != index:
+        raise ValueError(f"routing is on {routing.pair_row.device}, expected cuda:{index}")
 
 
 # a per-pair input gradient without a workspace computes the same sums in one piece;
@@ -535,47 +566,46 @@ def ace_moe_dx(dy, W, expert_routing: Routing, dx=None, input_mode: int = ACE_IN
     dx[t*k + j] = W_e^T dy[t*k + j], shared their sum over a token's slots.
     dx None allocates it (per pair: zeros, so that dropped pairs give 0)."""
     T, k = expert_routing.c.T, expert_routing.c.k
-    device = _on_device(W)
+    dev = _on_device(W)
     if W.dim() != 3:
         raise ValueError(f"W must be [E, d_out, d_in], got {tuple(W.shape)}")
     E, d_out, d_in = W.shape
-    dt = _dtype(W)
-    _check_routing(expert_routing, T, k, device)
-    _want("dy", dy, T * k * d_out, W.dtype, device)
+    dt = W.dtype
+    _check_routing(expert_routing, T, k, dev)
     shared = input_mode == ACE_INPUT_SHARED
     rows = T if shared else T * k
     if dx is None:
         if accumulate:
             raise ValueError("accumulate needs dx")
-        dx = _alloc(torch.empty if shared else torch.zeros, stream, rows, d_in, dtype=W.dtype,
-                    device=device)
-    _want("dx", dx, rows * d_in, W.dtype, device)
+        dx = _alloc(torch.empty if shared else torch.zeros, stream, rows, d_in, dtype=dt,
+                    device=W.device)
     if ws is None and (shared or accumulate or T * k * d_in <= _DX_SPLIT_ELEMS):
         need = ace_workspace_bytes(ACE_OP_MOE_DX, T, k, d_in, d_out, E, 0)
-        ws = _alloc(torch.empty, stream, max(need, 256), dtype=torch.uint8, device=device)
-    _want("ws", ws, None, torch.uint8, device, optional=True)
-    _check(_lib.ace_moe_dx(dt, input_mode, T, k, d_in, d_out, E, _ptr(dy), _ptr(W),
-                           ctypes.byref(expert_routing.c), int(accumulate), _ptr(dx), _ptr(ws),
-                           0 if ws is None else ws.numel(), _stream(stream)),
-           "ace_moe_dx")
+        ws = _alloc(torch.empty, stream, max(need, 256), dtype=torch.uint8, device=W.device)
+    ws_bytes = 0 if ws is None else ws.numel()
+    _check(_lib.ace_moe_dx(_dtype(W), input_mode, T, k, d_in, d_out, E,
+                           _arg("dy", dy, T * k * d_out, dt, dev),
+                           _arg("W", W, E * d_out * d_in, dt, dev), ctypes.byref(expert_routing.c),
+                           int(accumulate), _arg("dx", dx, rows * d_in, dt, dev),
+                           _opt("ws", ws, ws_bytes, torch.uint8, dev), ws_bytes,
+                           _stream_on(dev, stream)), "ace_moe_dx")
     return dx
 
 
 def ace_moe_combine_fwd(y, routing: Routing, out=None, pair_w=None, stream=None) -> torch.Tensor:
     """out[t] = sum over the routed slots j of pair_w[t, j] y[t*k + j]."""
     T, k = routing.c.T, routing.c.k
-    device = _on_device(y)
+    dev = _on_device(y)
     if y.dim() != 2 or y.shape[0] != T * k:
         raise ValueError(f"y must be [T*k={T * k}, d], got {tuple(y.shape)}")
-    d = y.shape[1]
-    dt = _dtype(y)
-    _check_routing(routing, T, k, device)
-    _want("pair_w", pair_w, T * k, torch.float32, device, optional=True)
+    d, dt = y.shape[1], y.dtype
+    _check_routing(routing, T, k, dev)
     if out is None:
-        out = _alloc(torch.empty, stream, T, d, dtype=y.dtype, device=device)
-    _want("out", out, T * d, y.dtype, device)
-    _check(_lib.ace_moe_combine_fwd(dt, T, k, d, _ptr(y), _ptr(pair_w), ctypes.byref(routing.c),
-                                    _ptr(out), _stream(stream)), "ace_moe_combine_fwd")
+        out = _alloc(torch.empty, stream, T, d, dtype=dt, device=y.device)
+    _check(_lib.ace_moe_combine_fwd(_dtype(y), T, k, d, _arg("y", y, T * k * d, dt, dev),
+                                    _opt("pair_w", pair_w, T * k, torch.float32, dev),
+                                    ctypes.byref(routing.c), _arg("out", out, T * d, dt, dev),
+                                    _stream_on(dev, stream)), "ace_moe_combine_fwd")
     return out
 
 
@@ -584,21 +614,19 @@ def ace_moe_combine_bwd(dout, routing: Routing, dy=None, pair_w=None, y=None, dw
     """dy[t*k + j] = pair_w[t, j] dout[t]; with dw also dw[t, j] = <dout[t], y[t*k + j]>.
     dy None allocates it (zeros, so that dropped pairs give 0)."""
     T, k = routing.c.T, routing.c.k
-    device = _on_device(dout)
+    dev = _on_device(dout)
     if dout.dim() != 2 or dout.shape[0] != T:
         raise ValueError(f"dout must be [T={T}, d], got {tuple(dout.shape)}")
-    d = dout.shape[1]
-    dt = _dtype(dout)
-    _check_routing(routing, T, k, device)
-    _want("pair_w", pair_w, T * k, torch.float32, device, optional=True)
-    _want("y", y, T * k * d, dout.dtype, device, optional=dw is None)
-    _want("dw", dw, T * k, torch.float32, device, optional=True)
+    d, dt = dout.shape[1], dout.dtype
+    _check_routing(routing, T, k, dev)
     if dy is None:
-        dy = _alloc(torch.zeros, stream, T * k, d, dtype=dout.dtype, device=device)
-    _want("dy", dy, T * k * d, dout.dtype, device)
-    _check(_lib.ace_moe_combine_bwd(dt, T, k, d, _ptr(dout), _ptr(y), _ptr(pair_w),
-                                    ctypes.byref(routing.c), _ptr(dy), _ptr(dw), _stream(stream)),
-           "ace_moe_combine_bwd")
+        dy = _alloc(torch.zeros, stream, T * k, d, dtype=dt, device=dout.device)
+    yp = _opt("y", y, T * k * d, dt, dev) if dw is None else _arg("y", y, T * k * d, dt, dev)
+    _check(_lib.ace_moe_combine_bwd(_dtype(dout), T, k, d, _arg("dout", dout, T * d, dt, dev), yp,
+                                    _opt("pair_w", pair_w, T * k, torch.float32, dev),
+                                    ctypes.byref(routing.c), _arg("dy", dy, T * k * d, dt, dev),
+                                    _opt("dw", dw, T * k, torch.float32, dev),
+                                    _stream_on(dev, stream)), "ace_moe_combine_bwd")
     return dy
 
 
@@ -613,26 +641,31 @@ class PackedAct:
         self.c = AcePackedAct(self.codes.data_ptr() or None, self.exps.data_ptr() or None)
 
 
-def _want_packed(name: str, c: PackedAct, rows: int, d: int, device) -> None:
+def _packed(name: str, c: PackedAct, rows: int, d: int, index: int):
+    """Checkpoint argument of the given shape and device."""
     if not isinstance(c, PackedAct):
         raise TypeError(f"{name} must be a PackedAct")
-    if (c.rows, c.d) != (rows, d):
+    if c.rows != rows or c.d != d:
         raise ValueError(f"{name} holds [{c.rows}, {c.d}], expected [{rows}, {d}]")
-    if c.codes.device != device:
-        raise ValueError(f"{name} is on {c.codes.device}, expected {device}")
+    if c.codes.get_device() != index:
+        raise ValueError(f"{name} is on {c.codes.device}, expected cuda:{index}")
+    return ctypes.byref(c.c)
+
+
+def _rows(name: str, t: torch.Tensor):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [rows, d], got {tuple(t.shape)}")
+    return t.shape
 
 
 def ace_act_pack(x, packed: Optional[PackedAct] = None, stream=None) -> PackedAct:
     """8-bit checkpoint of the rows x [rows, d] (include/ace.h)."""
-    device = _on_device(x)
-    if x.dim() != 2:
-        raise ValueError(f"x must be [rows, d], got {tuple(x.shape)}")
-    rows, d = x.shape
-    dt = _dtype(x)
+    dev = _on_device(x)
+    rows, d = _rows("x", x)
     if packed is None:
-        packed = _alloc(PackedAct, stream, rows, d, device=device)
-    _want_packed("packed", packed, rows, d, device)
-    _check(_lib.ace_act_pack(dt, rows, d, _ptr(x), ctypes.byref(packed.c), _stream(stream)),
+        packed = _alloc(PackedAct, stream, rows, d, device=x.device)
+    _check(_lib.ace_act_pack(_dtype(x), rows, d, _arg("x", x, rows * d, x.dtype, dev),
+                             _packed("packed", packed, rows, d, dev), _stream_on(dev, stream)),
            "ace_act_pack")
     return packed
 
@@ -640,30 +673,26 @@ def ace_act_pack(x, packed: Optional[PackedAct] = None, stream=None) -> PackedAc
 def ace_act_unpack(packed: PackedAct, x=None, dtype=None, stream=None) -> torch.Tensor:
     """The rows that a checkpoint stands for: into x, or a new tensor of dtype
     (bf16 by default; the values are exact in both types)."""
-    device = _on_device(packed.codes)
+    dev = _on_device(packed.codes)
     rows, d = packed.rows, packed.d
     if x is None:
-        x = _alloc(torch.empty, stream, rows, d, dtype=dtype or torch.bfloat16, device=device)
-    _want("x", x, rows * d, dtype, device)
-    _check(_lib.ace_act_unpack(_dtype(x), rows, d, ctypes.byref(packed.c), _ptr(x),
-                               _stream(stream)), "ace_act_unpack")
+        x = _alloc(torch.empty, stream, rows, d, dtype=dtype or torch.bfloat16,
+                   device=packed.codes.device)
+    _check(_lib.ace_act_unpack(_dtype(x), rows, d, _packed("packed", packed, rows, d, dev),
+                               _arg("x", x, rows * d, dtype or x.dtype, dev),
+                               _stream_on(dev, stream)), "ace_act_unpack")
     return x
 
 
-def _gate_up(g, u, rows: int, d: int, dtype, device):
+def _gate_up(g, u, rows: int, d: int, dtype, index: int):
     """(g, u, g_packed, u_packed) as the library takes them: pointers of the
     tensors, or None and the checkpoints."""
-    packed = isinstance(g, PackedAct)
-    if packed != isinstance(u, PackedAct):
+    if isinstance(g, PackedAct) != isinstance(u, PackedAct):
         raise TypeError("g and u must both be tensors or both be PackedAct")
-    for name, t in (("g", g), ("u", u)):
-        if packed:
-            _want_packed(name, t, rows, d, device)
-        else:
-            _want(name, t, rows * d, dtype, device)
-    if packed:
-        return None, None, ctypes.byref(g.c), ctypes.byref(u.c)
-    return _ptr(g), _ptr(u), None, None
+    if isinstance(g, PackedAct):
+        return None, None, _packed("g", g, rows, d, index), _packed("u", u, rows, d, index)
+    n = rows * d
+    return _arg("g", g, n, dtype, index), _arg("u", u, n, dtype, index), None, None
 
 
 def ace_swiglu_fwd(g, u, a=None, g_packed: Optional[PackedAct] = None,
@@ -671,45 +700,39 @@ def ace_swiglu_fwd(g, u, a=None, g_packed: Optional[PackedAct] = None,
     """a = g sigmoid(g) u per row.  g and u are tensors (with g_packed and
     u_packed their 8-bit checkpoints are written in the same pass) or both
     PackedAct (then a, or dtype, tells the type: bf16 by default)."""
-    packed = isinstance(g, PackedAct)
-    device = _on_device(g.codes if packed else g)
-    if not packed and g.dim() != 2:
-        raise ValueError(f"g must be [rows, d], got {tuple(g.shape)}")
-    rows, d = (g.rows, g.d) if packed else g.shape
-    if packed and (g_packed is not None or u_packed is not None):
+    held = isinstance(g, PackedAct)
+    src = g.codes if held else g
+    dev = _on_device(src)
+    rows, d = _rows("g", src)
+    if held and (g_packed is not None or u_packed is not None):
         raise ValueError("g and u are checkpoints already")
     if dtype is None:
-        dtype = g.dtype if not packed else a.dtype if a is not None else torch.bfloat16
-    gp, up, g8, u8 = _gate_up(g, u, rows, d, dtype, device)
+        dtype = g.dtype if not held else a.dtype if a is not None else torch.bfloat16
+    gp, up, g8, u8 = _gate_up(g, u, rows, d, dtype, dev)
     if a is None:
-        a = _alloc(torch.empty, stream, rows, d, dtype=dtype, device=device)
-    _want("a", a, rows * d, dtype, device)
-    for name, c in (("g_packed", g_packed), ("u_packed", u_packed)):
-        if c is not None:
-            _want_packed(name, c, rows, d, device)
+        a = _alloc(torch.empty, stream, rows, d, dtype=dtype, device=src.device)
     if g_packed is not None:
-        g8 = ctypes.byref(g_packed.c)
+        g8 = _packed("g_packed", g_packed, rows, d, dev)
     if u_packed is not None:
-        u8 = ctypes.byref(u_packed.c)
-    _check(_lib.ace_swiglu_fwd(_dtype(a), rows, d, gp, up, _ptr(a), g8, u8, _stream(stream)),
-           "ace_swiglu_fwd")
+        u8 = _packed("u_packed", u_packed, rows, d, dev)
+    _check(_lib.ace_swiglu_fwd(_dtype(a), rows, d, gp, up, _arg("a", a, rows * d, dtype, dev), g8,
+                               u8, _stream_on(dev, stream)), "ace_swiglu_fwd")
     return a
 
 
 def ace_swiglu_bwd(da, g, u, dg=None, du=None, stream=None):
     """(dg, du) of ace_swiglu_fwd; g and u are the forward's tensors or, both,
     their checkpoints (PackedAct)."""
-    device = _on_device(da)
-    if da.dim() != 2:
-        raise ValueError(f"da must be [rows, d], got {tuple(da.shape)}")
-    rows, d = da.shape
-    gp, up, g8, u8 = _gate_up(g, u, rows, d, da.dtype, device)
+    dev = _on_device(da)
+    rows, d = _rows("da", da)
+    dt = da.dtype
+    gp, up, g8, u8 = _gate_up(g, u, rows, d, dt, dev)
     if dg is None:
-        dg = _alloc(torch.empty, stream, rows, d, dtype=da.dtype, device=device)
+        dg = _alloc(torch.empty, stream, rows, d, dtype=dt, device=da.device)
     if du is None:
-        du = _alloc(torch.empty, stream, rows, d, dtype=da.dtype, device=device)
-    _want("dg", dg, rows * d, da.dtype, device)
-    _want("du", du, rows * d, da.dtype, device)
-    _check(_lib.ace_swiglu_bwd(_dtype(da), rows, d, _ptr(da), gp, up, g8, u8, _ptr(dg), _ptr(du),
-                               _stream(stream)), "ace_swiglu_bwd")
+        du = _alloc(torch.empty, stream, rows, d, dtype=dt, device=da.device)
+    n = rows * d
+    _check(_lib.ace_swiglu_bwd(_dtype(da), rows, d, _arg("da", da, n, dt, dev), gp, up, g8, u8,
+                               _arg("dg", dg, n, dt, dev), _arg("du", du, n, dt, dev),
+                               _stream_on(dev, stream)), "ace_swiglu_bwd")
     return dg, du
