@@ -13,7 +13,9 @@
 //     land.  (One block per tile spent about 14 us per tile outside its loop of
 //     14 to 28 us, with the matrix units and HBM busy in turns.)
 // A block's tiles are every 32nd of its XCD's run, so the blocks of an XCD work
-// on neighbouring tiles at a time.
+// on neighbouring tiles at a time.  Where the run's last round would occupy half
+// of the XCD's CUs or fewer, its tiles are cut into two or four column parts, which
+// as many blocks of a second set (launched behind the first) take.
 
 // Chunk swizzle of a 128-byte W^T row: pairs of chunks trade places, so that the
 // 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread
@@ -75,13 +77,16 @@ __device__ inline u32x2 round4(f32x4 v) {
 constexpr int kDxLargeK = 256;
 __device__ const u32x4 kZeros = {0u, 0u, 0u, 0u};
 
-template <bool RAGGED>
-__global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs a) {
+//
+// One block's tiles: NB 16-column blocks a wave (8: whole tiles, item, item + step,
+// ... below items; 4 or 2: part `item` of the halves or quarters of the tiles from
+// `items` on).  before, upto: see the kernel.
+template <bool RAGGED, int NB>
+__device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int before, int upto, int first, int item,
+                                          int step, int items) {
   using C = Large;
   using F = bf16x8;
-  constexpr int ROWB = C::ROWB, NC = C::COPIES, KPL = kMaxKeys / 64;
-  __shared__ __attribute__((aligned(16))) char smem[C::SLOTS * C::SLOT];
-
+  constexpr int ROWB = C::ROWB, NC = C::COPIES, KPL = kMaxKeys / 64, CW = 16 * NB;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, g = lane >> 4;
@@ -89,38 +94,16 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
   const int K = a.d_in, N = a.d_out;
   const int nst = (K + C::KC - 1) / C::KC, nst2 = (nst + 1) & ~1;
 
-  // ---- tiles.  Lane l keeps the number of tiles before and up to the end of
-  // the keys KPL l .. KPL l + KPL - 1.
-  int before, upto;
-  {
-    int cnt = 0, off[KPL + 1];
-#pragma unroll
-    for (int i = 0; i <= KPL; ++i) off[i] = a.offsets[min(lane * KPL + i, a.E)];
-#pragma unroll
-    for (int i = 0; i < KPL; ++i) cnt += (off[i + 1] - off[i] + C::BM - 1) / C::BM * a.nt;
-    upto = cnt;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
-    }
-    before = upto - cnt;
-  }
-  const int n_tiles = __builtin_amdgcn_readfirstlane(__shfl(upto, 63, 64));
-  const int per_xcd = (n_tiles + kXcds - 1) / kXcds;
-  const int xcd = blockIdx.x % kXcds, step = gridDim.x / kXcds;
-  int tile = xcd * per_xcd + blockIdx.x / kXcds;
-  const int tile_end = min((xcd + 1) * per_xcd, n_tiles);
-  if (tile >= tile_end) return;
-
   struct Tile {
-    int e, n0, u0, hi;   // expert, first column, first row, end of the expert's rows
+    int e, n0, u0, hi;   // expert, first column (a part's may lie past the last),
+                         // first row, end of the expert's rows
   };
   // (offsets through the constant address space: scalar loads, which the copies
   // in flight do not hold up); within an expert, groups of up to eight row tiles
   // walk the columns together
   const auto soff = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.offsets;
-  auto locate = [&](int t) {
+  auto locate = [&](int it) {
+    const int t = first + (NB == 8 ? it : items + it / (8 / NB));
     const int owner = __builtin_ctzll(__ballot(t >= before && t < upto));
     int rem = t - __builtin_amdgcn_readlane(before, owner), q = owner * KPL;
     int lo = soff[q], hi = soff[min(q + 1, a.E)];
@@ -135,18 +118,19 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
     const int m_e = (hi - lo + C::BM - 1) / C::BM;
     const int grp = rem / (kRowGroup * a.nt), gsz = min(kRowGroup, m_e - grp * kRowGroup);
     const int ing = rem - grp * kRowGroup * a.nt;
-    return Tile{q, ing / gsz * C::BN, lo + (grp * kRowGroup + ing % gsz) * C::BM, hi};
+    const int n0 = ing / gsz * C::BN + (NB == 8 ? 0 : it % (8 / NB) * 2 * CW);
+    return Tile{q, n0, lo + (grp * kRowGroup + ing % gsz) * C::BM, hi};
   };
   // pairs of the wave's rows 128 wy + lane and + 64 (past the segment: its last)
   auto pairs = [&](const Tile& t, int (&p)[2]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) p[i] = a.pair_list[min(t.u0 + 128 * wy + 64 * i + lane, t.hi - 1)];
   };
-  Tile cur = locate(tile), nxt = cur;
+  Tile cur = locate(item), nxt = cur;
   int pc[2], pn[2];      // pairs of the current and the next tile
   pairs(cur, pc);
-  bool more = tile + step < tile_end;
-  if (more) nxt = locate(tile + step);
+  bool more = NB == 8 && item + step < items;
+  if (more) nxt = locate(item + step);
   pairs(nxt, pn);
 
   // ---- copies: the waves wx = 0 copy the x rows of their wy, the others the W
@@ -158,15 +142,16 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
   uint32_t roff[2][NC];    // slots P[v] of even and of odd v
   const char* base;        // x, or the tile's first column of W_e
   auto set_tile = [&](const Tile& t, const int (&p)[2]) {
+    const int n0 = min(t.n0, N - 8);
     base = xwave ? static_cast<const char*>(a.x)
-                 : static_cast<const char*>(a.W) + ((size_t)t.e * K * N + t.n0) * 2;
+                 : static_cast<const char*>(a.W) + ((size_t)t.e * K * N + n0) * 2;
 #pragma unroll
     for (int par = 0; par < 2; ++par)
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
         const int h = xwave ? 1 - par : par;   // x unit v + 1, W unit v + 2
-        const int c = 16 * wy + 8 * h + (cpos ^ lt_swz(8 * i + crl));
-        const uint32_t w = (uint32_t)(8 * i + crl) * (uint32_t)(N / 8) + min(c, (N - t.n0) / 8 - 1);
+        const int c = CW / 8 * wy + 8 * h + (cpos ^ lt_swz(8 * i + crl));
+        const uint32_t w = (uint32_t)(8 * i + crl) * (uint32_t)(N / 8) + min(c, (N - n0) / 8 - 1);
         const uint32_t x = (uint32_t)__shfl(p[h], 8 * i + crl, 64) * (uint32_t)(K / 8);
         roff[par][i] = xwave ? x : w;
       }
@@ -222,9 +207,9 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
   }
 
   F x0[4], x1a[4], x1b[4], wa[16], wb[16];   // x: K-block 0 and 1 of a half, W: [nb + 8 kh]
-  f32x4 acc[8][8];
+  f32x4 acc[NB][8];
 #pragma unroll
-  for (int nb = 0; nb < 8; ++nb)
+  for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
     for (int mb = 0; mb < 8; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
@@ -271,11 +256,11 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
     for (int i = 0; i < 16; ++i) {
       if (i < 8) {
         if (i < 4) x1n[i] = *reinterpret_cast<const F*>(xs1 + i * 16 * ROWB);
-        wn[4 * PAR + (i & 3) + 8 * (i >> 2)] = wt_read(i & 3, i >> 2);
+        if (4 * PAR + (i & 3) < NB) wn[4 * PAR + (i & 3) + 8 * (i >> 2)] = wt_read(i & 3, i >> 2);
         copy(PAR, i);
       }
       if (i >= 8 && i < 12) x0[i - 8] = *reinterpret_cast<const F*>(xs + (i - 8) * 16 * ROWB);
-      if constexpr (MMA) {
+      if (MMA && (i & 7) < NB) {
 #pragma unroll
         for (int mb = 0; mb < 4; ++mb) {
           const int nb = i & 7, kh = i >> 3;
@@ -307,9 +292,9 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
     const bool last = !more;
     Tile nn = nxt;
     int pnn[2];
-    tile += step;
-    more = tile + step < tile_end;
-    if (more) nn = locate(tile + step);
+    item += step;
+    more = NB == 8 && item + step < items;
+    if (more) nn = locate(item + step);
     pairs(nn, pnn);
     mfma_done();
     __builtin_amdgcn_sched_barrier(0);
@@ -317,15 +302,15 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
     // blocks the lanes of a row trade their 8-byte pieces until lane g holds the
     // 16 bytes g: a store covers 64 bytes of each of 16 rows (32 bytes of them:
     // 35 us more for 134 MB of results).
-    const int col0 = cur.n0 + 128 * wx + 8 * g;
+    const int col0 = cur.n0 + CW * wx + 8 * g;
 #pragma unroll
     for (int mb = 0; mb < 8; ++mb) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int nb = 0; nb < 8; ++nb) asm volatile("" : "+a"(acc[nb][mb]));   // read behind mfma_done
-      u32x4 o[4];
+      for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+a"(acc[nb][mb]));   // read behind mfma_done
+      u32x4 o[NB / 2];
 #pragma unroll
-      for (int nb = 0; nb < 8; nb += 2) {
+      for (int nb = 0; nb < NB; nb += 2) {
         u32x2 lo = round4(acc[nb][mb]), hi = round4(acc[nb + 1][mb]);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -339,11 +324,11 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
       if (cur.u0 + 128 * wy + 16 * mb + c16 < cur.hi) {
         __bf16* row = Y + (size_t)p * N + col0;
 #pragma unroll
-        for (int nb = 0; nb < 8; nb += 2)
+        for (int nb = 0; nb < NB; nb += 2)
           if (col0 + 16 * nb < N) *reinterpret_cast<u32x4*>(row + 16 * nb) = o[nb / 2];
       }
 #pragma unroll
-      for (int nb = 0; nb < 8; ++nb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int nb = 0; nb < NB; ++nb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     if (last) break;
     // the loads above are older than the stores: a use here waits for them only,
@@ -359,6 +344,42 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
     }
   }
   wait_vmcnt<0>();   // copies past the last tile (repeats of its last stage)
+}
+
+template <bool RAGGED>
+__global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs a) {
+  using C = Large;
+  constexpr int KPL = kMaxKeys / 64;
+  __shared__ __attribute__((aligned(16))) char smem[C::SLOTS * C::SLOT];
+  // Lane l keeps the number of tiles before and up to the end of the keys KPL l ..
+  // KPL l + KPL - 1.
+  const int lane = threadIdx.x & 63;
+  int cnt = 0, off[KPL + 1];
+#pragma unroll
+  for (int i = 0; i <= KPL; ++i) off[i] = a.offsets[min(lane * KPL + i, a.E)];
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) cnt += (off[i + 1] - off[i] + C::BM - 1) / C::BM * a.nt;
+  int upto = cnt;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += v;
+  }
+  const int before = upto - cnt;
+  // the XCD's run of tiles, and how many of them form a last round that is cut up
+  const int n_tiles = __builtin_amdgcn_readfirstlane(__shfl(upto, 63, 64));
+  const int per_xcd = (n_tiles + kXcds - 1) / kXcds;
+  const int step = gridDim.x / (2 * kXcds);     // blocks of each set per XCD
+  const int first = blockIdx.x % kXcds * per_xcd, mine = max(0, min(per_xcd, n_tiles - first));
+  const int over = mine % step, whole = 2 * over <= step ? mine - over : mine;
+  const int b = blockIdx.x / kXcds;
+  if (b < step) {
+    if (b < whole) moe_dx_large_block<RAGGED, 8>(a, smem, before, upto, first, b, step, whole);
+  } else if (4 * over <= step) {
+    if (b - step < 4 * (mine - whole)) moe_dx_large_block<RAGGED, 2>(a, smem, before, upto, first, b - step, step, whole);
+  } else {
+    if (b - step < 2 * (mine - whole)) moe_dx_large_block<RAGGED, 4>(a, smem, before, upto, first, b - step, step, whole);
+  }
 }
 
 // ---- few rows per expert: the weights bound the call, and a block streams them.

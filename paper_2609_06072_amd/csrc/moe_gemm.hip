@@ -845,10 +845,10 @@ hipError_t launch_moe_dx_large(MoeArgs a, long P, hipStream_t stream) {
   a.nt = (a.d_out + Large::BN - 1) / Large::BN;
   const long max_tiles = ((P + Large::BM - 1) / Large::BM + a.E) * a.nt;
   if (max_tiles > 0x7fffffffL - 4096) return hipErrorInvalidConfiguration;
-  // one block per CU, the same number for each XCD
+  // two sets of one block per CU, the same number for each XCD
   const int cus = (device_cu_count() + kXcds - 1) / kXcds * kXcds;
-  if (a.d_in % (2 * Large::KC) != 0) moe_dx_large_kernel<true><<<cus, Large::THREADS, 0, stream>>>(a);
-  else moe_dx_large_kernel<false><<<cus, Large::THREADS, 0, stream>>>(a);
+  if (a.d_in % (2 * Large::KC) != 0) moe_dx_large_kernel<true><<<2 * cus, Large::THREADS, 0, stream>>>(a);
+  else moe_dx_large_kernel<false><<<2 * cus, Large::THREADS, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -103,6 +103,8 @@ DX_SIZES = [
     (40, 3, 4, 72, 2056, 0.2, 0.0),
     (1300, 2, 8, 264, 328, 0.02, 0.8),      # a ragged contraction in large tiles
     (700, 2, 2, 1096, 384, 0.0, 0.0),
+    (2600, 2, 2, 1032, 264, 0.0, 0.0),      # 110 large tiles: in halves
+    (4000, 2, 2, 2056, 256, 0.0, 0.0),      # 288: a round, then quarters
 ]
 
 
