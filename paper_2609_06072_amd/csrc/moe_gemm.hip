@@ -911,34 +911,36 @@ bool mid_f32(const MoeArgs& a, long P) {
 namespace {
 
 // The input gradient: which kernel.  The number of tiles of bm x bn is estimated
-// from the average number of rows per expert (half a tile lost in each; the host
-// does not know the routing), one for every expert that can be hit at least.
+// from the average number of rows per expert (half a tile lost in each that can be
+// hit; the host does not know the routing), one for each of these at least.
 enum DxKernel { kDxS16x64, kDxS32x64, kDxS64x64, kDxS32x128, kDxS64x128, kDxTiles, kDxLarge };
 
 long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
-  const long hit = P < a.E ? P : a.E, rows = P / bm + a.E / 2;
+  const long hit = P < a.E ? P : a.E, rows = P / bm + hit / 2;
   return (rows > hit ? rows : hit) * ((a.d_out + bn - 1) / bn);
 }
 
-// bf16.  Two estimates, of rounds of blocks over the CUs (K the contraction):
-//   large tiles  a round of 8 us + 24 us per 1000 of K (20 where no stage is ragged)
-//   streaming, 64 rows x 128 columns (one block per CU)   4 us + 9.5 us per 1000
+// bf16.  Two estimates, of rounds of blocks over the CUs (us; K the contraction
+// in thousands):
+//   large tiles  8 + 29 K a round; a last one that is cut up, 6 + 19 K in halves and
+//                6 + 16 K in quarters
+//   streaming, 64 rows x 128 columns (one block per CU)   4 + 9.5 K
 // decide between the two (us a call, measured 64 x 128 / large, random routings,
 // weights out of every cache):
 //   K, columns, experts     rows per expert
-//   2048, 1024, 64           32    56 /  64        64    87 /  68      100   117 /  71
-//   4096, 4096, 8            64    88 /  94       128   128 /  93
-//   14336, 4096, 8           64   263 / 312       128   543 / 343
-//   1000, 2056, 16           64    35 /  40       128    65 /  43
+//   2048, 1024, 64           32    58 /  70        64    87 /  69      100   117 /  71
+//   4096, 4096, 8            32    53 /  76        64    91 /  74      128   128 /  93
+//   14336, 4096, 8           32   161 / 249        64   317 / 253      128   543 / 343
+//   1000, 2056, 16           64    38 /  37        96    50 /  38
 //   304, 3232, 16            20    15 /  20       100    31 /  22
-//   616, 336, 32            200    26 /  26       600    54 /  29
-//   5032, 456, 16           444   138 / 141      1000   282 / 145
-//   1568, 424, 4            981    23 /  49      2000    42 /  50
-//   512, 256, 8            1000    10 /  20      4000    35 /  22
+//   616, 336, 32            100    15 /  17       200    26 /  18
+//   5032, 456, 16           200    79 /  93       444   137 /  99
+//   1568, 424, 4            981    23 /  32      2000    42 /  35
+//   512, 256, 8             500    10 /  12      1000    16 /  13
 // Among the streaming forms (32 x 64 / 64 x 64 / 32 x 128 / 64 x 128), the first
-// that fits the chip once (CUs; 1.25 CUs for 64 x 64, of which two share one), and
-// 128 columns beyond:
+// that fits the CUs once, and 128 columns beyond:
 //   1568, 424, 4             20    13 /  13 /  17 /  18     300    26 /  19 /  17 /  21
+//                           600     - /  34 /   - /  22
 //   8944, 792, 8             20    64 /  64 /  82 /  83     100   160 /  92 / 112 / 115
 //   1024, 1024, 16           16     9 /  10 /  11 /  12      64    18 /  17 /  18 /  15
 //   2048, 1024, 64           16    55 /  55 /  49 /  51      32     - /   - /  69 /  56
@@ -947,12 +949,13 @@ constexpr long kDxStream32 = 20;
 
 DxKernel dx_kernel_bf16(const MoeArgs& a, long P) {
   const long cus = device_cu_count(), K = a.d_in;
-  auto rounds = [&](long blocks) { return (blocks + cus - 1) / cus; };
-  const long large = rounds(dx_blocks(a, P, Large::BM, Large::BN)) * (8000 + (K % (2 * Large::KC) ? 24 : 20) * K);
-  const long stream = rounds(dx_blocks(a, P, 64, 128)) * (8000 + 19 * K) / 2;
+  const long tiles = dx_blocks(a, P, Large::BM, Large::BN), over = tiles % cus;
+  const long round = 8000 + 29 * K, last = over == 0 ? 0 : 4 * over <= cus ? 6000 + 16 * K : 2 * over <= cus ? 6000 + 19 * K : round;
+  const long large = tiles / cus * round + last;
+  const long stream = (dx_blocks(a, P, 64, 128) + cus - 1) / cus * (8000 + 19 * K) / 2;
   if (K >= kDxLargeK && P > kDxStream32 * a.E && large < stream) return kDxLarge;
   if (dx_blocks(a, P, 32, 64) <= cus) return kDxS32x64;
-  if (4 * dx_blocks(a, P, 64, 64) <= 5 * cus) return kDxS64x64;
+  if (dx_blocks(a, P, 64, 64) <= cus) return kDxS64x64;
   return P <= kDxStream32 * a.E ? kDxS32x128 : kDxS64x128;
 }
 
