@@ -821,13 +821,14 @@ hipError_t launch_moe_large(MoeArgs a, long P, bool wide, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, int NRB, int BN>
+template <typename T, int NRB, int BN, bool RUNS>
 hipError_t launch_moe_dx_stream(MoeArgs a, long P, hipStream_t stream) {
   using C = DxStream<T, NRB, BN>;
   a.nt = (a.d_out + C::BN - 1) / C::BN;
-  const long grid = ((P + C::BM - 1) / C::BM + a.E) * a.nt * a.splits;
+  const long max_items = ((P + C::BM - 1) / C::BM + a.E) * a.nt * a.splits;
+  const long grid = (max_items + kXcds - 1) / kXcds * kXcds;
   if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
-  moe_dx_stream_kernel<T, NRB, BN><<<(int)grid, 256, 0, stream>>>(a);
+  moe_dx_stream_kernel<T, NRB, BN, RUNS><<<(int)grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -1003,16 +1004,21 @@ int moe_dx_splits(int dtype, const MoeArgs& a, long P) {
 
 hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream) {
   const DxKernel k = dx_kernel(dtype, a, P);
+  const bool runs32 = P > 32L * a.E, runs64 = P > 64L * a.E;   // several row tiles per expert
   if (dtype == ACE_F32) {
-    if (k == kDxS16x64) return launch_moe_dx_stream<float, 1, 64>(a, P, stream);
-    if (k == kDxS32x64) return launch_moe_dx_stream<float, 2, 64>(a, P, stream);
-    if (k == kDxS64x64) return launch_moe_dx_stream<float, 4, 64>(a, P, stream);
+    if (k == kDxS16x64) return launch_moe_dx_stream<float, 1, 64, false>(a, P, stream);
+    if (k == kDxS32x64 && !runs32) return launch_moe_dx_stream<float, 2, 64, false>(a, P, stream);
+    if (k == kDxS32x64) return launch_moe_dx_stream<float, 2, 64, true>(a, P, stream);
+    if (k == kDxS64x64) return launch_moe_dx_stream<float, 4, 64, true>(a, P, stream);
     return launch_moe_dx_tile(a, P, stream);
   }
-  if (k == kDxS32x64) return launch_moe_dx_stream<__bf16, 2, 64>(a, P, stream);
-  if (k == kDxS64x64) return launch_moe_dx_stream<__bf16, 4, 64>(a, P, stream);
-  if (k == kDxS32x128) return launch_moe_dx_stream<__bf16, 2, 128>(a, P, stream);
-  if (k == kDxS64x128) return launch_moe_dx_stream<__bf16, 4, 128>(a, P, stream);
+  if (k == kDxS32x64 && !runs32) return launch_moe_dx_stream<__bf16, 2, 64, false>(a, P, stream);
+  if (k == kDxS32x64) return launch_moe_dx_stream<__bf16, 2, 64, true>(a, P, stream);
+  if (k == kDxS64x64 && !runs64) return launch_moe_dx_stream<__bf16, 4, 64, false>(a, P, stream);
+  if (k == kDxS64x64) return launch_moe_dx_stream<__bf16, 4, 64, true>(a, P, stream);
+  if (k == kDxS32x128) return launch_moe_dx_stream<__bf16, 2, 128, false>(a, P, stream);
+  if (k == kDxS64x128 && !runs64) return launch_moe_dx_stream<__bf16, 4, 128, false>(a, P, stream);
+  if (k == kDxS64x128) return launch_moe_dx_stream<__bf16, 4, 128, true>(a, P, stream);
   return launch_moe_dx_large(a, P, stream);
 }
 

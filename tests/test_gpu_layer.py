@@ -105,6 +105,12 @@ DX_SIZES = [
     (700, 2, 2, 1096, 384, 0.0, 0.0),
     (2600, 2, 2, 1032, 264, 0.0, 0.0),      # 110 large tiles: in halves
     (4000, 2, 2, 2056, 256, 0.0, 0.0),      # 288: a round, then quarters
+    (320, 2, 64, 320, 72, 0.0, 0.0),        # the streaming forms: 32 x 128,
+    (1000, 2, 64, 328, 136, 0.0, 0.8),      # 64 x 128,
+    (1000, 2, 4, 520, 136, 0.05, 0.0),      # with several row tiles per expert,
+    (750, 2, 32, 328, 136, 0.0, 0.0),       # 64 x 64,
+    (800, 2, 8, 328, 136, 0.0, 0.8),        # with several row tiles
+    (1030, 2, 2, 1920, 72, 0.0, 0.0),       # fp32 tiles
 ]
 
 
