@@ -986,9 +986,18 @@ DxKernel dx_kernel(int dtype, const MoeArgs& a, long P) {
 
 }  // namespace
 
-// A block of the narrow forms takes 4 us per 1000 of the contraction, 31 GB/s of
-// weights on its CU; the join costs 3 us more.  (9816 x 544, 4 experts, 1 row each:
-// 43 us in one.)
+// Blocks per tile of the narrow forms: as many as fill the chip once (fp32, whose
+// matrix work is longer: twice), each with 640 (fp32: 320) of the contraction at
+// least; the join takes the place of the sum over slots, or 2 us more per pair.
+// us a call, shared input (1 / 2 / 4 / 8 blocks a tile):
+//   bf16  9816 x 544, 4 experts, 16 pairs      47.1 / 29.1 / 20.6 / 21.1
+//         2000 x 304, 8, 240                   21.2 / 16.1 / 15.6 / 19.4
+//         1504 x 1000, 8, 80                   16.5 / 14.1 / 15.1 / 18.8
+//         1024 x 512, 8, 512                   11.3 / 11.6 / 12.6 / 18.8
+//   fp32  4952 x 296, 64, 6                    50.9 / 29.9 / 20.1 / 16.1
+//         1568 x 424, 4, 200                   27.7 / 18.8 / 15.1 / 18.1
+//         1024 x 512, 8, 512                   20.4 / 19.6 / 18.7 / 23.4 (3: 17.3)
+//         1012 x 1924, 4, 132                  22.2 / 22.7 / 27.2 / 34.6
 int moe_dx_splits(int dtype, const MoeArgs& a, long P) {
   if (P * a.d_out > kDxSplitElems) return 1;
   long bm;
@@ -998,8 +1007,9 @@ int moe_dx_splits(int dtype, const MoeArgs& a, long P) {
     case kDxS64x64: bm = 64; break;
     default: return 1;
   }
-  const long s = device_cu_count() / dx_blocks(a, P, bm, 64), most = a.d_in / 1024;
-  return (int)std::max(1L, std::min({s, most, (long)kDxMaxSplits}));
+  const bool f32 = dtype == ACE_F32;
+  const long fill = (f32 ? 2L : 1L) * device_cu_count() / dx_blocks(a, P, bm, 64), most = a.d_in / (f32 ? 320 : 640);
+  return (int)std::max(1L, std::min({fill, most, (long)kDxMaxSplits}));
 }
 
 hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream) {
