@@ -331,12 +331,13 @@ ace_status ace_moe_lora_fwd(ace_dtype dtype, ace_input_mode input_mode, int32_t 
  *               ace_workspace_bytes(ACE_OP_MOE_DX, T, k, d_in, d_out, E, 0)
  *               where it holds a row of dtype per pair (the products are summed
  *               in fp32 and rounded to dtype there; a token's rows are then
- *               added in fp32, in slot order, and rounded once), or, in small
- *               calls, fp32 sums over parts of a contraction that several
- *               blocks share.  May be NULL for the per-pair input with
- *               accumulate = 0: then no contraction is shared.  No
- *               initialisation.
- * Limits: T * k * d_out and T * k * d_in below 2^33 - 4096, d_in below 2^24.
+ *               added in fp32, in slot order, and rounded once; with k = 1 the
+ *               row is the result), or, in calls of few tiles, fp32 sums over
+ *               parts of a contraction that several blocks share.  May be NULL
+ *               for the per-pair input with accumulate = 0: then no contraction
+ *               is shared.  No initialisation.
+ * Limits: T * k * d_out and T * k * d_in below 2^33 - 4096, d_in below 2^24,
+ * d_out below 2^30.
  * Deterministic.
  */
 ace_status ace_moe_dx(ace_dtype dtype, ace_input_mode input_mode, int32_t T, int32_t k,

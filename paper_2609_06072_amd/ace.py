@@ -556,8 +556,8 @@ def _check_routing(routing: Routing, T: int, k: int, index: int) -> None:
 
 
 # a per-pair input gradient without a workspace computes the same sums in one piece;
-# small calls are given one
-_DX_SPLIT_ELEMS = 1 << 19
+# calls up to this size are given one
+_DX_SPLIT_ELEMS = 1 << 22
 
 
 def ace_moe_dx(dy, W, expert_routing: Routing, dx=None, input_mode: int = ACE_INPUT_SHARED,

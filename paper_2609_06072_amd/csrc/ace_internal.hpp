@@ -130,13 +130,16 @@ hipError_t launch_moe_gemm(int dtype, const MoeArgs& a, long P, hipStream_t stre
 // The input gradient of the expert projection, y[p] = W_e^T x[p] per pair: x is
 // the output's gradient [T*k][d_in], W [E][d_in][d_out] (d_in, d_out: the
 // product's own contraction length and columns), per_pair, no adapter.
-hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream);
-// Blocks that share a tile of that product (1: a.y is written; otherwise a.part,
-// [splits][P][d_out] fp32, to be joined).  At most kDxMaxSplits, and 1 where P *
-// d_out passes kDxSplitElems.
-constexpr int kDxMaxSplits = 8;
-constexpr long kDxSplitElems = 1L << 19;
-int moe_dx_splits(int dtype, const MoeArgs& a, long P);
+enum DxKernel { kDxS16x64, kDxS32x64, kDxS64x64, kDxS32x128, kDxS64x128, kDxTiles, kDxLarge };
+struct DxPlan {
+  DxKernel kernel;
+  int splits;   // blocks that share a tile's contraction (1: a.y is written; otherwise
+                // a.part, [splits][P][d_out] fp32, to be joined)
+};
+// At most so many for a result of `elems` elements.
+constexpr long dx_max_splits(long elems) { return elems <= 1L << 19 ? 8 : elems <= 1L << 22 ? 4 : 1; }
+DxPlan moe_dx_plan(int dtype, const MoeArgs& a, long P, bool may_split);
+hipError_t launch_moe_dx(int dtype, DxPlan plan, const MoeArgs& a, long P, hipStream_t stream);
 struct DxJoinArgs {
   const float* part;          // [splits][pairs][d]
   const int32_t* pair_row;
@@ -160,6 +163,8 @@ struct CombineArgs {
   uint32_t pieces;
 };
 hipError_t launch_combine_fwd(int dtype, CombineArgs a, int T, hipStream_t stream);
+// Zeros in the rows [T][d] of out whose pair was dropped (one pair per token).
+hipError_t launch_zero_dropped(int dtype, const int32_t* pair_row, int T, int d, void* out, hipStream_t stream);
 struct CombineBwdArgs {
   const void* dout;           // [T][d]
   const void* y;              // [T*k][d], read for dw only

@@ -298,7 +298,7 @@ constexpr int64_t kMaxRowElems = ((int64_t)1 << 33) - 4096;
 
 size_t moe_dx_ws_bytes(int T, int k, int d_in) {
   const size_t rows = (size_t)T * k * d_in;
-  return rows * (rows <= (size_t)kDxSplitElems ? kDxMaxSplits : 1) * sizeof(float);
+  return rows * dx_max_splits((long)rows) * sizeof(float);
 }
 
 ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, int32_t d_in,
@@ -319,7 +319,8 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   if (E < 1 || E > kMaxKeys) return fail(ACE_ERR_UNSUPPORTED, "E = %d outside [1, %d]", E, kMaxKeys);
   if ((int64_t)E * d_out * d_in >= (int64_t)1 << 40)
     return fail(ACE_ERR_UNSUPPORTED, "expert weights too large");
-  if (d_in >= 1 << 24) return fail(ACE_ERR_UNSUPPORTED, "d_in = %d, at most 2^24 - 1", d_in);
+  if (d_in >= 1 << 24 || d_out >= 1 << 30)
+    return fail(ACE_ERR_UNSUPPORTED, "d_in = %d (below 2^24), d_out = %d (below 2^30)", d_in, d_out);
   if ((int64_t)T * k * d_out >= kMaxRowElems || (int64_t)T * k * d_in >= kMaxRowElems)
     return fail(ACE_ERR_UNSUPPORTED, "T*k*d_out or T*k*d_in reaches 2^33 elements");
   if (accumulate != 0 && accumulate != 1) return fail(ACE_ERR_INVALID_ARG, "accumulate = %d", accumulate);
@@ -355,12 +356,15 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   a.d_in = d_out;    // the product contracts over the projection's outputs
   a.d_out = d_in;
   a.per_pair = 1;
-  a.y = pair_rows ? ws : dx;
   const long P = (long)T * k;
   a.pairs = P;
-  a.splits = ws ? moe_dx_splits(dtype, a, P) : 1;
+  const DxPlan plan = moe_dx_plan(dtype, a, P, ws != nullptr);
+  a.splits = plan.splits;
   a.part = static_cast<float*>(ws);
-  hipError_t e = launch_moe_dx(dtype, a, P, st);
+  // one pair per token: its row is the token's
+  const bool rows_are_tokens = im == ACE_INPUT_SHARED && k == 1 && !accumulate;
+  a.y = pair_rows && !rows_are_tokens ? ws : dx;
+  hipError_t e = launch_moe_dx(dtype, plan, a, P, st);
   if (e == hipSuccess && a.splits > 1) {
     DxJoinArgs j{};
     j.part = a.part;
@@ -374,6 +378,8 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
     j.keep = im == ACE_INPUT_PER_PAIR;
     return hip_status(launch_moe_dx_join(dtype, j, st), "input gradient join launch");
   }
+  if (e == hipSuccess && rows_are_tokens)
+    return hip_status(launch_zero_dropped(dtype, ert->pair_row, T, d_in, dx, st), "input gradient launch");
   if (e != hipSuccess || !pair_rows) return hip_status(e, "input gradient launch");
   // the token's rows, or (per pair) each row as a token of its own
   CombineArgs c{};

@@ -82,7 +82,23 @@ __global__ __launch_bounds__(kThreads) void combine_bwd_kernel(CombineBwdArgs a)
   }
 }
 
+// One wave per row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void zero_dropped_kernel(const int32_t* pair_row, int T_, int d, T* out) {
+  const int t = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (t >= T_ || pair_row[t] >= 0) return;
+  for (int c = (threadIdx.x & 63) * Tr<T>::PER; c < d; c += 64 * Tr<T>::PER)
+    Tr<T>::store(out + (size_t)t * d + c, Tr<T>::zero());
+}
+
 }  // namespace
+
+hipError_t launch_zero_dropped(int dtype, const int32_t* pair_row, int T, int d, void* out, hipStream_t stream) {
+  const int grid = (T + kThreads / 64 - 1) / (kThreads / 64);
+  if (dtype == ACE_BF16) zero_dropped_kernel<__bf16><<<grid, kThreads, 0, stream>>>(pair_row, T, d, static_cast<__bf16*>(out));
+  else zero_dropped_kernel<float><<<grid, kThreads, 0, stream>>>(pair_row, T, d, static_cast<float*>(out));
+  return hipGetLastError();
+}
 
 hipError_t launch_combine_fwd(int dtype, CombineArgs a, int T, hipStream_t stream) {
   const int per = dtype == ACE_BF16 ? 8 : 4;

@@ -15,7 +15,9 @@
 // A block's tiles are every 32nd of its XCD's run, so the blocks of an XCD work
 // on neighbouring tiles at a time.  Where the run's last round would occupy half
 // of the XCD's CUs or fewer, its tiles are cut into two or four column parts, which
-// as many blocks of a second set (launched behind the first) take.
+// as many blocks of a second set (launched behind the first) take.  With splits,
+// that many blocks share a tile's contraction (a tile below is then one of these
+// parts) and store fp32 sums for moe_dx_join_kernel.
 
 // Chunk swizzle of a 128-byte W^T row: pairs of chunks trade places, so that the
 // 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread
@@ -92,11 +94,13 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
   const int c16 = lane & 15, g = lane >> 4;
   const int wy = wave >> 1, wx = wave & 1;
   const int K = a.d_in, N = a.d_out;
-  const int nst = (K + C::KC - 1) / C::KC, nst2 = (nst + 1) & ~1;
+  // stages of a tile (an even number; RAGGED: those past the contraction are zeros)
+  const int nst2 = 2 * ((K + 2 * C::KC * a.splits - 1) / (2 * C::KC * a.splits));
 
   struct Tile {
     int e, n0, u0, hi;   // expert, first column (a part's may lie past the last),
                          // first row, end of the expert's rows
+    int split;
   };
   // (offsets through the constant address space: scalar loads, which the copies
   // in flight do not hold up); within an expert, groups of up to eight row tiles
@@ -108,7 +112,7 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
     int rem = t - __builtin_amdgcn_readlane(before, owner), q = owner * KPL;
     int lo = soff[q], hi = soff[min(q + 1, a.E)];
     for (;;) {   // at most KPL keys
-      const int n = (hi - lo + C::BM - 1) / C::BM * a.nt;
+      const int n = (hi - lo + C::BM - 1) / C::BM * a.nt * a.splits;
       if (rem < n) break;
       rem -= n;
       ++q;
@@ -116,10 +120,12 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
       hi = soff[min(q + 1, a.E)];
     }
     const int m_e = (hi - lo + C::BM - 1) / C::BM;
+    const int split = rem / (m_e * a.nt);
+    rem -= split * m_e * a.nt;
     const int grp = rem / (kRowGroup * a.nt), gsz = min(kRowGroup, m_e - grp * kRowGroup);
     const int ing = rem - grp * kRowGroup * a.nt;
     const int n0 = ing / gsz * C::BN + (NB == 8 ? 0 : it % (8 / NB) * 2 * CW);
-    return Tile{q, n0, lo + (grp * kRowGroup + ing % gsz) * C::BM, hi};
+    return Tile{q, n0, lo + (grp * kRowGroup + ing % gsz) * C::BM, hi, split};
   };
   // pairs of the wave's rows 128 wy + lane and + 64 (past the segment: its last)
   auto pairs = [&](const Tile& t, int (&p)[2]) {
@@ -141,8 +147,10 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
   const int col[2] = {cpos ^ l_swz(crl), cpos ^ l_swz(8 + crl)};
   uint32_t roff[2][NC];    // slots P[v] of even and of odd v
   const char* base;        // x, or the tile's first column of W_e
+  int st0;                 // the tile's first stage of the contraction
   auto set_tile = [&](const Tile& t, const int (&p)[2]) {
     const int n0 = min(t.n0, N - 8);
+    st0 = t.split * nst2;
     base = xwave ? static_cast<const char*>(a.x)
                  : static_cast<const char*>(a.W) + ((size_t)t.e * K * N + n0) * 2;
 #pragma unroll
@@ -177,7 +185,7 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
       set_tile(nxt, pn);
     }
     // (a block without a next tile repeats its last stage)
-    const int st = max(0, min(cst, nst2 - 1));
+    const int st = st0 + max(0, min(cst, nst2 - 1));
     if (xwave) {
       sbase = base;
 #pragma unroll
@@ -302,7 +310,8 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
     // blocks the lanes of a row trade their 8-byte pieces until lane g holds the
     // 16 bytes g: a store covers 64 bytes of each of 16 rows (32 bytes of them:
     // 35 us more for 134 MB of results).
-    const int col0 = cur.n0 + CW * wx + 8 * g;
+    // With splits the fp32 sums go out as they are.
+    const int col0 = cur.n0 + CW * wx + 8 * g, col1 = cur.n0 + CW * wx + 4 * g;
 #pragma unroll
     for (int mb = 0; mb < 8; ++mb) {
       __builtin_amdgcn_sched_barrier(0);
@@ -321,7 +330,14 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
         }
       }
       const int p = __shfl(pc[mb >> 2], 16 * (mb & 3) + c16, 64);
-      if (cur.u0 + 128 * wy + 16 * mb + c16 < cur.hi) {
+      if (a.splits > 1) {
+        if (cur.u0 + 128 * wy + 16 * mb + c16 < cur.hi) {
+          float* row = a.part + ((size_t)cur.split * a.pairs + p) * N + col1;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            if (col1 + 16 * nb < N) *reinterpret_cast<f32x4*>(row + 16 * nb) = acc[nb][mb];
+        }
+      } else if (cur.u0 + 128 * wy + 16 * mb + c16 < cur.hi) {
         __bf16* row = Y + (size_t)p * N + col0;
 #pragma unroll
         for (int nb = 0; nb < NB; nb += 2)
@@ -358,7 +374,7 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
 #pragma unroll
   for (int i = 0; i <= KPL; ++i) off[i] = a.offsets[min(lane * KPL + i, a.E)];
 #pragma unroll
-  for (int i = 0; i < KPL; ++i) cnt += (off[i + 1] - off[i] + C::BM - 1) / C::BM * a.nt;
+  for (int i = 0; i < KPL; ++i) cnt += (off[i + 1] - off[i] + C::BM - 1) / C::BM * a.nt * a.splits;
   int upto = cnt;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {

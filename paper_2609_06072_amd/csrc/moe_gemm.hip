@@ -844,11 +844,11 @@ hipError_t launch_moe_dx_tile(MoeArgs a, long P, hipStream_t stream) {
 
 hipError_t launch_moe_dx_large(MoeArgs a, long P, hipStream_t stream) {
   a.nt = (a.d_out + Large::BN - 1) / Large::BN;
-  const long max_tiles = ((P + Large::BM - 1) / Large::BM + a.E) * a.nt;
+  const long max_tiles = ((P + Large::BM - 1) / Large::BM + a.E) * a.nt * a.splits;
   if (max_tiles > 0x7fffffffL - 4096) return hipErrorInvalidConfiguration;
   // two sets of one block per CU, the same number for each XCD
   const int cus = (device_cu_count() + kXcds - 1) / kXcds * kXcds;
-  if (a.d_in % (2 * Large::KC) != 0) moe_dx_large_kernel<true><<<2 * cus, Large::THREADS, 0, stream>>>(a);
+  if (a.d_in % (2 * Large::KC * a.splits) != 0) moe_dx_large_kernel<true><<<2 * cus, Large::THREADS, 0, stream>>>(a);
   else moe_dx_large_kernel<false><<<2 * cus, Large::THREADS, 0, stream>>>(a);
   return hipGetLastError();
 }
@@ -914,7 +914,6 @@ namespace {
 // The input gradient: which kernel.  The number of tiles of bm x bn is estimated
 // from the average number of rows per expert (half a tile lost in each that can be
 // hit; the host does not know the routing), one for each of these at least.
-enum DxKernel { kDxS16x64, kDxS32x64, kDxS64x64, kDxS32x128, kDxS64x128, kDxTiles, kDxLarge };
 
 long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
   const long hit = P < a.E ? P : a.E, rows = P / bm + hit / 2;
@@ -926,8 +925,10 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //   large tiles  8 + 29 K a round; a last one that is cut up, 6 + 19 K in halves and
 //                6 + 16 K in quarters
 //   streaming, 64 rows x 128 columns (one block per CU)   4 + 9.5 K
-// decide between the two (us a call, measured 64 x 128 / large, random routings,
-// weights out of every cache):
+//   32 x 64 and 64 x 64 where they fit the CUs once       4 + 4.5 K and 4 + 6 K
+// and where blocks share a contraction 3 more (large tiles: also their sums at 5
+// TB/s), decide between large tiles and streaming.  us a call, measured 64 x 128 /
+// large, random routings, weights out of every cache, contractions not shared:
 //   K, columns, experts     rows per expert
 //   2048, 1024, 64           32    58 /  70        64    87 /  69      100   117 /  71
 //   4096, 4096, 8            32    53 /  76        64    91 /  74      128   128 /  93
@@ -938,6 +939,10 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //   5032, 456, 16           200    79 /  93       444   137 /  99
 //   1568, 424, 4            981    23 /  32      2000    42 /  35
 //   512, 256, 8             500    10 /  12      1000    16 /  13
+// Large tiles, one block for a contraction / as many as estimated best:
+//   7784, 912, 16           164   178 / 121
+//   6728, 568, 32           147   151 / 125
+//   5624, 336, 64           130   125 / 113
 // Among the streaming forms (32 x 64 / 64 x 64 / 32 x 128 / 64 x 128), the first
 // that fits the CUs once, and 128 columns beyond:
 //   1568, 424, 4             20    13 /  13 /  17 /  18     300    26 /  19 /  17 /  21
@@ -947,44 +952,6 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //   2048, 1024, 64           16    55 /  55 /  49 /  51      32     - /   - /  69 /  56
 //   14336, 4096, 8           16     - / 164 / 152 / 152      32     - / 190 / 268 / 161
 constexpr long kDxStream32 = 20;
-
-DxKernel dx_kernel_bf16(const MoeArgs& a, long P) {
-  const long cus = device_cu_count(), K = a.d_in;
-  const long tiles = dx_blocks(a, P, Large::BM, Large::BN), over = tiles % cus;
-  const long round = 8000 + 29 * K, last = over == 0 ? 0 : 4 * over <= cus ? 6000 + 16 * K : 2 * over <= cus ? 6000 + 19 * K : round;
-  const long large = tiles / cus * round + last;
-  const long stream = (dx_blocks(a, P, 64, 128) + cus - 1) / cus * (8000 + 19 * K) / 2;
-  if (K >= kDxLargeK && P > kDxStream32 * a.E && large < stream) return kDxLarge;
-  if (dx_blocks(a, P, 32, 64) <= cus) return kDxS32x64;
-  if (dx_blocks(a, P, 64, 64) <= cus) return kDxS64x64;
-  return P <= kDxStream32 * a.E ? kDxS32x128 : kDxS64x128;
-}
-
-// fp32: streaming with 16, 32 and 64 rows (64 columns), tiles, us a call:
-//   1024, 512, 8            64    18 /  17 /  24 /  89
-//   2048, 1024, 64           4    92 / 101 / 160 / 297      16   133 / 105 / 157 / 298
-//                           64   359 / 263 / 267 / 298     200   865 / 620 / 584 / 572
-//   1024, 2048, 16         128   139 / 115 / 119 / 152     600   562 / 435 / 392 / 419
-//                         1200  1099 / 836 / 757 / 696
-// From 128 rows on by rounds of tiles: a CU works through its tiles at the rate of
-// its matrix units, 10% faster per element than the streaming kernel, whose small
-// blocks even out.  Both count half a tile lost per expert.
-constexpr long kDxStream16F32 = 8, kDxStream32F32 = 128;
-
-DxKernel dx_kernel_f32(const MoeArgs& a, long P) {
-  if (P <= kDxStream16F32 * a.E) return kDxS16x64;
-  if (P <= kDxStream32F32 * a.E) return kDxS32x64;
-  const long cus = device_cu_count(), BM = DxTile::BM, BN = DxTile::BN;
-  const long tiles = (P / BM + a.E / 2) * ((a.d_out + BN - 1) / BN);
-  const bool ahead = 9 * ((tiles + cus - 1) / cus * cus) * BM * BN < 10 * (P + 32 * (long)a.E) * a.d_out;
-  return ahead ? kDxTiles : kDxS64x64;
-}
-
-DxKernel dx_kernel(int dtype, const MoeArgs& a, long P) {
-  return dtype == ACE_F32 ? dx_kernel_f32(a, P) : dx_kernel_bf16(a, P);
-}
-
-}  // namespace
 
 // Blocks per tile of the narrow forms: as many as fill the chip once (fp32, whose
 // matrix work is longer: twice), each with 640 (fp32: 320) of the contraction at
@@ -998,22 +965,65 @@ DxKernel dx_kernel(int dtype, const MoeArgs& a, long P) {
 //         1568 x 424, 4, 200                   27.7 / 18.8 / 15.1 / 18.1
 //         1024 x 512, 8, 512                   20.4 / 19.6 / 18.7 / 23.4 (3: 17.3)
 //         1012 x 1924, 4, 132                  22.2 / 22.7 / 27.2 / 34.6
-int moe_dx_splits(int dtype, const MoeArgs& a, long P) {
-  if (P * a.d_out > kDxSplitElems) return 1;
-  long bm;
-  switch (dx_kernel(dtype, a, P)) {
-    case kDxS16x64: bm = 16; break;
-    case kDxS32x64: bm = 32; break;
-    case kDxS64x64: bm = 64; break;
-    default: return 1;
-  }
-  const bool f32 = dtype == ACE_F32;
+DxPlan dx_narrow(bool f32, DxKernel kernel, const MoeArgs& a, long P, bool may_split) {
+  const long bm = kernel == kDxS16x64 ? 16 : kernel == kDxS32x64 ? 32 : 64;
   const long fill = (f32 ? 2L : 1L) * device_cu_count() / dx_blocks(a, P, bm, 64), most = a.d_in / (f32 ? 320 : 640);
-  return (int)std::max(1L, std::min({fill, most, (long)kDxMaxSplits}));
+  return {kernel, may_split ? (int)std::max(1L, std::min({fill, most, dx_max_splits(P * a.d_out)})) : 1};
 }
 
-hipError_t launch_moe_dx(int dtype, const MoeArgs& a, long P, hipStream_t stream) {
-  const DxKernel k = dx_kernel(dtype, a, P);
+DxPlan dx_plan_bf16(const MoeArgs& a, long P, bool may_split) {
+  const long cus = device_cu_count(), K = a.d_in;
+  const long tiles = dx_blocks(a, P, Large::BM, Large::BN);
+  long large = -1;   // ns
+  int splits = 1;
+  for (int s = 1; s <= (may_split ? dx_max_splits(P * a.d_out) : 1) && K / s >= kDxLargeK; ++s) {
+    const long over = tiles * s % cus, Ks = K / s;
+    const long round = 8000 + 29 * Ks;
+    const long last = over == 0 ? 0 : 4 * over <= cus ? 6000 + 16 * Ks : 2 * over <= cus ? 6000 + 19 * Ks : round;
+    const long t = tiles * s / cus * round + last + (s > 1 ? 3000 + s * P * a.d_out * 8 / 5000 : 0);
+    if (large < 0 || t < large) {
+      large = t;
+      splits = s;
+    }
+  }
+  DxPlan stream{P <= kDxStream32 * a.E ? kDxS32x128 : kDxS64x128, 1};
+  long t = (dx_blocks(a, P, 64, 128) + cus - 1) / cus * (8000 + 19 * K) / 2;
+  const bool fit32 = dx_blocks(a, P, 32, 64) <= cus;
+  if (fit32 || dx_blocks(a, P, 64, 64) <= cus) {
+    stream = dx_narrow(false, fit32 ? kDxS32x64 : kDxS64x64, a, P, may_split);
+    t = 4000 + (fit32 ? 9 : 12) * K / 2 / stream.splits + (stream.splits > 1 ? 3000 : 0);
+  }
+  return large >= 0 && P > kDxStream32 * a.E && large < t ? DxPlan{kDxLarge, splits} : stream;
+}
+
+// fp32: streaming with 16, 32 and 64 rows (64 columns), tiles, us a call:
+//   1024, 512, 8            64    18 /  17 /  24 /  89
+//   2048, 1024, 64           4    92 / 101 / 160 / 297      16   133 / 105 / 157 / 298
+//                           64   359 / 263 / 267 / 298     200   865 / 620 / 584 / 572
+//   1024, 2048, 16         128   139 / 115 / 119 / 152     600   562 / 435 / 392 / 419
+//                         1200  1099 / 836 / 757 / 696
+// From 128 rows on by rounds of tiles: a CU works through its tiles at the rate of
+// its matrix units, 10% faster per element than the streaming kernel, whose small
+// blocks even out.  Both count half a tile lost per expert.
+constexpr long kDxStream16F32 = 8, kDxStream32F32 = 128;
+
+DxPlan dx_plan_f32(const MoeArgs& a, long P, bool may_split) {
+  if (P <= kDxStream16F32 * a.E) return dx_narrow(true, kDxS16x64, a, P, may_split);
+  if (P <= kDxStream32F32 * a.E) return dx_narrow(true, kDxS32x64, a, P, may_split);
+  const long cus = device_cu_count(), BM = DxTile::BM, BN = DxTile::BN;
+  const long tiles = (P / BM + a.E / 2) * ((a.d_out + BN - 1) / BN);
+  const bool ahead = 9 * ((tiles + cus - 1) / cus * cus) * BM * BN < 10 * (P + 32 * (long)a.E) * a.d_out;
+  return ahead ? DxPlan{kDxTiles, 1} : dx_narrow(true, kDxS64x64, a, P, may_split);
+}
+
+}  // namespace
+
+DxPlan moe_dx_plan(int dtype, const MoeArgs& a, long P, bool may_split) {
+  return dtype == ACE_F32 ? dx_plan_f32(a, P, may_split) : dx_plan_bf16(a, P, may_split);
+}
+
+hipError_t launch_moe_dx(int dtype, DxPlan plan, const MoeArgs& a, long P, hipStream_t stream) {
+  const DxKernel k = plan.kernel;
   const bool runs32 = P > 32L * a.E, runs64 = P > 64L * a.E;   // several row tiles per expert
   if (dtype == ACE_F32) {
     if (k == kDxS16x64) return launch_moe_dx_stream<float, 1, 64, false>(a, P, stream);

@@ -34,7 +34,7 @@ INV, UNS, WSP = -1, -2, -3
     (dict(k=0), UNS), (dict(k=33), UNS), (dict(T=1 << 30, k=4), UNS),
     (dict(d_in=60), UNS), (dict(d_out=36), UNS), (dict(dt=0, d_in=62), UNS),
     (dict(d_in=0), INV), (dict(d_out=-8), INV), (dict(E=0), UNS), (dict(E=257), UNS),
-    (dict(d_in=1 << 24), UNS), (dict(T=1 << 20, k=2, d_out=4096), UNS),
+    (dict(d_in=1 << 24), UNS), (dict(d_out=1 << 30, E=1, d_in=8, T=1, k=1, rt=dict(n_keys=1)), UNS), (dict(T=1 << 20, k=2, d_out=4096), UNS),
     (dict(T=1 << 20, k=2, d_in=4096), UNS), (dict(d_in=1 << 20, d_out=1 << 20), UNS),
     (dict(acc=2), INV), (dict(rt=None), INV), (dict(E=3), INV),
     (dict(rt=dict(mode=0)), INV), (dict(rt=dict(T=5)), INV), (dict(rt=dict(pair_row=None)), INV),

@@ -111,6 +111,10 @@ DX_SIZES = [
     (750, 2, 32, 328, 136, 0.0, 0.0),       # 64 x 64,
     (800, 2, 8, 328, 136, 0.0, 0.8),        # with several row tiles
     (1030, 2, 2, 1920, 72, 0.0, 0.0),       # fp32 tiles
+    (1500, 1, 3, 520, 264, 0.1, 0.0),       # one pair per token, some dropped
+    (600, 2, 2, 264, 2056, 0.05, 0.0),      # large tiles that share contractions,
+    (600, 2, 2, 264, 2048, 0.05, 0.0),      # whole stages each,
+    (2500, 1, 1, 1000, 4200, 0.0, 0.0),     # in parts and several a block
 ]
 
 
