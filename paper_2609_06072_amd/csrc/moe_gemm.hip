@@ -920,12 +920,13 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
   return (rows > hit ? rows : hit) * ((a.d_out + bn - 1) / bn);
 }
 
-// bf16.  Two estimates, of rounds of blocks over the CUs (us; K the contraction
-// in thousands):
+// bf16.  Estimates of rounds of blocks over the CUs (us; K the contraction in
+// thousands, 5 for the call):
 //   large tiles  8 + 29 K a round; a last one that is cut up, 6 + 19 K in halves and
 //                6 + 16 K in quarters
-//   streaming, 64 rows x 128 columns (one block per CU)   4 + 9.5 K
-//   32 x 64 and 64 x 64 where they fit the CUs once       4 + 4.5 K and 4 + 6 K
+//   streaming, 64 rows x 128 columns (one block per CU)   4 + 9.5 K a round
+//   64 x 64, two blocks per CU, for short contractions    2.3 + 3 K per CU's block
+//   32 x 64 and 64 x 64 where they fit the CUs once       4 + 4.5 K and 4 + 6 K in all
 // and where blocks share a contraction 3 more (large tiles: also their sums at 5
 // TB/s), decide between large tiles and streaming.  us a call, measured 64 x 128 /
 // large, random routings, weights out of every cache, contractions not shared:
@@ -951,7 +952,13 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //   1024, 1024, 16           16     9 /  10 /  11 /  12      64    18 /  17 /  18 /  15
 //   2048, 1024, 64           16    55 /  55 /  49 /  51      32     - /   - /  69 /  56
 //   14336, 4096, 8           16     - / 164 / 152 / 152      32     - / 190 / 268 / 161
-constexpr long kDxStream32 = 20;
+// and for short contractions 64 columns there, two blocks or three per CU:
+//   264, 496, 96             40    14 /  16 /  19 /  18      75    19 /  21 /  25 /  24
+//   264, 2048, 16           100    16 /  15 /  16 /  17     400    44 /  42 /  45 /  51
+//   544, 296, 64             64    11 /  17 /  18 /  21
+//   512, 1024, 64            64    31 /  32 /  32 /  31     128    46 /  43 /  47 /  46
+//   1024, 1024, 64           64    48 /  53 /  57 /  49
+constexpr long kDxStream32 = 20, kDxShortK = 640, kDxShort32 = 80;
 
 // Blocks per tile of the narrow forms: as many as fill the chip once (fp32, whose
 // matrix work is longer: twice), each with 640 (fp32: 320) of the contraction at
@@ -974,7 +981,7 @@ DxPlan dx_narrow(bool f32, DxKernel kernel, const MoeArgs& a, long P, bool may_s
 DxPlan dx_plan_bf16(const MoeArgs& a, long P, bool may_split) {
   const long cus = device_cu_count(), K = a.d_in;
   const long tiles = dx_blocks(a, P, Large::BM, Large::BN);
-  long large = -1;   // ns
+  long large = -1;   // ns, without the call's 5
   int splits = 1;
   for (int s = 1; s <= (may_split ? dx_max_splits(P * a.d_out) : 1) && K / s >= kDxLargeK; ++s) {
     const long over = tiles * s % cus, Ks = K / s;
@@ -988,10 +995,14 @@ DxPlan dx_plan_bf16(const MoeArgs& a, long P, bool may_split) {
   }
   DxPlan stream{P <= kDxStream32 * a.E ? kDxS32x128 : kDxS64x128, 1};
   long t = (dx_blocks(a, P, 64, 128) + cus - 1) / cus * (8000 + 19 * K) / 2;
+  const long blocks = dx_blocks(a, P, 64, 64);
   const bool fit32 = dx_blocks(a, P, 32, 64) <= cus;
-  if (fit32 || dx_blocks(a, P, 64, 64) <= cus) {
+  if (fit32 || blocks <= cus) {
     stream = dx_narrow(false, fit32 ? kDxS32x64 : kDxS64x64, a, P, may_split);
-    t = 4000 + (fit32 ? 9 : 12) * K / 2 / stream.splits + (stream.splits > 1 ? 3000 : 0);
+    t = -1000 + (fit32 ? 9 : 12) * K / 2 / stream.splits + (stream.splits > 1 ? 3000 : 0);
+  } else if (K <= kDxShortK && P > kDxStream32 * a.E) {
+    stream = {P <= kDxShort32 * a.E ? kDxS32x64 : kDxS64x64, 1};
+    t = blocks * (2300 + 3 * K) / cus;
   }
   return large >= 0 && P > kDxStream32 * a.E && large < t ? DxPlan{kDxLarge, splits} : stream;
 }
