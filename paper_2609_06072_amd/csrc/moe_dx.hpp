@@ -72,6 +72,13 @@ __device__ inline u32x2 round4(f32x4 v) {
   return __builtin_bit_cast(u32x2, bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]});
 }
 
+// The lane's number, computed where it is asked for.
+__device__ inline int lane_id() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 // RAGGED: K is no multiple of two stages; the copies of chunks past it read
 // zeros instead (both operands': an infinity times zero is no zero).  Zeroing the
 // fragments instead cost 0.6 of 1.8 us a stage on the one wave of a SIMD.
@@ -104,17 +111,19 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
   };
   // (offsets through the constant address space: scalar loads, which the copies
   // in flight do not hold up); within an expert, groups of up to eight row tiles
-  // walk the columns together
+  // walk the columns together.  The search goes on from the last tile's key, q.
   const auto soff = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.offsets;
+  auto tile_of = [&](int it) { return first + (NB == 8 ? it : items + it / (8 / NB)); };
+  const int owner = __builtin_ctzll(__ballot(tile_of(item) >= before && tile_of(item) < upto));
+  int q = owner * KPL, key0 = __builtin_amdgcn_readlane(before, owner);   // the key's first tile
+  int lo = soff[q], hi = soff[min(q + 1, a.E)];
   auto locate = [&](int it) {
-    const int t = first + (NB == 8 ? it : items + it / (8 / NB));
-    const int owner = __builtin_ctzll(__ballot(t >= before && t < upto));
-    int rem = t - __builtin_amdgcn_readlane(before, owner), q = owner * KPL;
-    int lo = soff[q], hi = soff[min(q + 1, a.E)];
-    for (;;) {   // at most KPL keys
+    int rem = tile_of(it) - key0;
+    for (;;) {   // ends: the tile is one of the offsets' tiles
       const int n = (hi - lo + C::BM - 1) / C::BM * a.nt * a.splits;
       if (rem < n) break;
       rem -= n;
+      key0 += n;
       ++q;
       lo = hi;
       hi = soff[min(q + 1, a.E)];
@@ -122,15 +131,18 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
     const int m_e = (hi - lo + C::BM - 1) / C::BM;
     const int split = rem / (m_e * a.nt);
     rem -= split * m_e * a.nt;
-    const int grp = rem / (kRowGroup * a.nt), gsz = min(kRowGroup, m_e - grp * kRowGroup);
-    const int ing = rem - grp * kRowGroup * a.nt;
+    int gtiles = kRowGroup * a.nt;
+    asm volatile("" : "+s"(gtiles));   // (its reciprocal, kept, would be spilled)
+    const int grp = rem / gtiles, gsz = min(kRowGroup, m_e - grp * kRowGroup);
+    const int ing = rem - grp * gtiles;
     const int n0 = ing / gsz * C::BN + (NB == 8 ? 0 : it % (8 / NB) * 2 * CW);
     return Tile{q, n0, lo + (grp * kRowGroup + ing % gsz) * C::BM, hi, split};
   };
   // pairs of the wave's rows 128 wy + lane and + 64 (past the segment: its last)
   auto pairs = [&](const Tile& t, int (&p)[2]) {
+    const int r = t.u0 + 128 * wy + lane_id();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p[i] = a.pair_list[min(t.u0 + 128 * wy + 64 * i + lane, t.hi - 1)];
+    for (int i = 0; i < 2; ++i) p[i] = a.pair_list[min(r + 64 * i, t.hi - 1)];
   };
   Tile cur = locate(item), nxt = cur;
   int pc[2], pn[2];      // pairs of the current and the next tile
@@ -138,12 +150,14 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
   bool more = NB == 8 && item + step < items;
   if (more) nxt = locate(item + step);
   pairs(nxt, pn);
+  asm volatile("" : "+v"(pn[0]), "+v"(pn[1]));   // waits here, and not in the loop
 
   // ---- copies: the waves wx = 0 copy the x rows of their wy, the others the W
   // columns of the half wy: of a slot eight 8-row copies, lane l the chunk at
   // position l & 7 of row l >> 3.  Offsets count 16-byte chunks.
   const int crl = lane >> 3, cpos = lane & 7;
   const bool xwave = wx == 0;
+  const int xmask = xwave ? -1 : 0;
   const int col[2] = {cpos ^ l_swz(crl), cpos ^ l_swz(8 + crl)};
   uint32_t roff[2][NC];    // slots P[v] of even and of odd v
   const char* base;        // x, or the tile's first column of W_e
@@ -160,7 +174,8 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
         const int h = xwave ? 1 - par : par;   // x unit v + 1, W unit v + 2
         const int c = CW / 8 * wy + 8 * h + (cpos ^ lt_swz(8 * i + crl));
         const uint32_t w = (uint32_t)(8 * i + crl) * (uint32_t)(N / 8) + min(c, (N - n0) / 8 - 1);
-        const uint32_t x = (uint32_t)__shfl(p[h], 8 * i + crl, 64) * (uint32_t)(K / 8);
+        // (p[h], as an indexed array would lie in memory)
+        const uint32_t x = (uint32_t)__shfl(p[par] ^ ((p[0] ^ p[1]) & xmask), 8 * i + crl, 64) * (uint32_t)(K / 8);
         roff[par][i] = xwave ? x : w;
       }
   };
@@ -246,13 +261,13 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
   // The copies come to the end of the tile in its last stage but two, an odd one.
   // drained: the first four half-steps behind a tile whose 32 stores were all
   // issued.  The slots they read were copied before the stores, which may all be
-  // under way.  (Any other order has 24 copies behind the needed ones.)
+  // under way beside the 24 copies behind the needed ones.
   auto half = [&](auto par_c, auto mma_c, auto odd_c, bool drained, F (&x1)[4], F (&wc)[16], F (&x1n)[4], F (&wn)[16]) {
     constexpr int PAR = decltype(par_c)::value;
     constexpr bool MMA = decltype(mma_c)::value;
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-    if (drained) wait_vmcnt<32>();
+    if (drained) wait_vmcnt<56>();
     else wait_vmcnt<24>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -311,9 +326,14 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
     // 16 bytes g: a store covers 64 bytes of each of 16 rows (32 bytes of them:
     // 35 us more for 134 MB of results).
     // With splits the fp32 sums go out as they are.
-    const int col0 = cur.n0 + CW * wx + 8 * g, col1 = cur.n0 + CW * wx + 4 * g;
-#pragma unroll
-    for (int mb = 0; mb < 8; ++mb) {
+    // full: all 32 stores are issued, in a straight line, so that the compiler can
+    // count them where it waits for the loads above, which are older.
+    // (the lane's number anew: kept, it and what follows from it would be spilled,
+    // and a reload waits for the copies in flight)
+    const int ln = lane_id(), lc16 = ln & 15, lg = ln >> 4;
+    const int col0 = cur.n0 + CW * wx + 8 * lg, col1 = cur.n0 + CW * wx + 4 * lg, row0 = cur.u0 + 128 * wy + lc16;
+    auto store = [&](auto full_c, int mb) {
+      constexpr bool FULL = decltype(full_c)::value;
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+a"(acc[nb][mb]));   // read behind mfma_done
@@ -329,28 +349,34 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
           o[nb / 2][2 + i] = s[1];
         }
       }
-      const int p = __shfl(pc[mb >> 2], 16 * (mb & 3) + c16, 64);
-      if (a.splits > 1) {
-        if (cur.u0 + 128 * wy + 16 * mb + c16 < cur.hi) {
+      const int p = __shfl(pc[mb >> 2], 16 * (mb & 3) + lc16, 64);
+      if (!FULL && a.splits > 1) {
+        if (row0 + 16 * mb < cur.hi) {
           float* row = a.part + ((size_t)cur.split * a.pairs + p) * N + col1;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
             if (col1 + 16 * nb < N) *reinterpret_cast<f32x4*>(row + 16 * nb) = acc[nb][mb];
         }
-      } else if (cur.u0 + 128 * wy + 16 * mb + c16 < cur.hi) {
+      } else if (FULL || row0 + 16 * mb < cur.hi) {
         __bf16* row = Y + (size_t)p * N + col0;
 #pragma unroll
         for (int nb = 0; nb < NB; nb += 2)
-          if (col0 + 16 * nb < N) *reinterpret_cast<u32x4*>(row + 16 * nb) = o[nb / 2];
+          if (FULL || col0 + 16 * nb < N) *reinterpret_cast<u32x4*>(row + 16 * nb) = o[nb / 2];
       }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    drained = NB == 8 && a.splits == 1 && cur.u0 + C::BM <= cur.hi && cur.n0 + C::BN <= N;
+    if (drained) {
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb) store(Yes{}, mb);
+      asm volatile("" : "+v"(pnn[0]), "+v"(pnn[1]));
+    } else {
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb) store(No{}, mb);
+      asm volatile("" : "+v"(pnn[0]), "+v"(pnn[1]));
     }
     if (last) break;
-    // the loads above are older than the stores: a use here waits for them only,
-    // one further on would wait for the copies as well
-    asm volatile("" : "+v"(pnn[0]), "+v"(pnn[1]));
-    drained = cur.u0 + C::BM <= cur.hi && cur.n0 + C::BN <= N;
     cur = nxt;
     nxt = nn;
 #pragma unroll
