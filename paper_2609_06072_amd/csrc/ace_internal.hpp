@@ -146,7 +146,7 @@ struct DxJoinArgs {
   void* out;                  // [pairs / k][d]
   long pairs;
   int32_t splits, k, d, accumulate;
-  int32_t keep;               // k == 1: rows of dropped pairs are left alone
+  int32_t keep;               // 1: rows without a routed pair are left alone
   FastDiv per_row;            // (set by the launcher)
   uint32_t pieces;
 };

@@ -26,9 +26,11 @@ __global__ __launch_bounds__(kThreads) void combine_fwd_kernel(CombineArgs a) {
   float acc[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.f;
+  bool routed = false;
   for (int j = 0; j < a.k; ++j) {
     const size_t p = (size_t)t * a.k + j;
     if (a.pair_row[p] < 0) continue;
+    routed = true;
     const float w = a.pair_w ? a.pair_w[p] : 1.f;
     float v[PER];
     Tr<T>::to_f32(Tr<T>::load_nt(Y + p * a.d + pc), v);
@@ -36,6 +38,7 @@ __global__ __launch_bounds__(kThreads) void combine_fwd_kernel(CombineArgs a) {
     for (int i = 0; i < PER; ++i) acc[i] += w * v[i];
   }
   if (a.accumulate) {
+    if (!routed) return;   // (a sum with 0 would lose a zero's sign)
     float v[PER];
     Tr<T>::to_f32(Tr<T>::load(out), v);
 #pragma unroll

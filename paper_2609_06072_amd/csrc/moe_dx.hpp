@@ -584,14 +584,14 @@ __global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
   if (idx >= a.pieces) return;
   const uint32_t t = a.per_row.div(idx), col = 4 * (idx - t * a.per_row.d);
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  bool routed = false;
   for (int j = 0; j < a.k; ++j) {
     const size_t p = (size_t)t * a.k + j;
-    if (a.pair_row[p] < 0) {
-      if (a.k == 1 && a.keep) return;   // a dropped pair's own row is left alone
-      continue;
-    }
+    if (a.pair_row[p] < 0) continue;
+    routed = true;
     for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(a.part + ((size_t)s * a.pairs + p) * a.d + col);
   }
+  if (!routed && (a.keep || a.accumulate)) return;   // (a sum with 0 would lose a zero's sign)
   T4* out = reinterpret_cast<T4*>(static_cast<T*>(a.out) + (size_t)t * a.d + col);
   if (a.accumulate) {
     const T4 o = *out;

@@ -115,6 +115,12 @@ DX_SIZES = [
     (600, 2, 2, 264, 2056, 0.05, 0.0),      # large tiles that share contractions,
     (600, 2, 2, 264, 2048, 0.05, 0.0),      # whole stages each,
     (2500, 1, 1, 1000, 4200, 0.0, 0.0),     # in parts and several a block
+    (3000, 2, 16, 264, 1536, 0.0, 0.8),     # large tiles, two blocks a contraction,
+    (3000, 2, 16, 264, 1544, 0.05, 0.0),    # ragged
+    (3000, 4, 200, 256, 1024, 0.05, 0.8),   # large tiles of many experts
+    (2600, 2, 2, 1024, 256, 0.0, 0.0),      # whole stages, in halves
+    (1000, 2, 64, 264, 648, 0.0, 0.0),      # 64 x 128 streaming,
+    (1200, 2, 32, 504, 648, 0.0, 0.0),      # with several row tiles
 ]
 
 
@@ -175,6 +181,43 @@ def test_moe_dx_infinities_stay_in_their_rows(ace, dtype):
         ref, tol = dx_refs(f64(torch.nan_to_num(dy, posinf=0)), f64(torch.nan_to_num(W, posinf=0)), ids, E, dtype, False)
         keep = clean.cpu().numpy()
         close("finite rows", f64(dx)[keep], ref[keep], tol[keep])
+
+
+def test_moe_dx_infinities_in_large_tiles(ace):
+    """The same where tiles of 256 rows share a ragged contraction: its end is
+    filled with zeros on both sides."""
+    T, k, E, d_in, d_out = 6000, 1, 16, 264, 1544
+    ids = (np.arange(T, dtype=np.int32) % E).reshape(T, 1)
+    rt = route(ace, ids, E)
+    dy, W = gen(6, T, d_out), gen(7, E, d_out, d_in)
+    W[2, d_out - 1, :] = float("inf")
+    W[3, 0, :] = float("nan")
+    dy[5, :] = float("inf")
+    dy[21, d_out - 1] = float("nan")
+    dx = ace.ace_moe_dx(dy, W, rt, input_mode=ace.ACE_INPUT_PER_PAIR)
+    t = np.arange(T)
+    clean = torch.from_numpy(~np.isin(ids[:, 0], (2, 3)) & ~np.isin(t, (5, 21))).cuda()
+    assert bool(torch.isfinite(dx[clean]).all())
+    assert not bool(torch.isfinite(dx[~clean]).any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,k,d", [(40, 2, 72), (40, 1, 72), (900, 2, 520)])
+def test_moe_dx_leaves_what_no_pair_reaches(ace, dtype, T, k, d):
+    """Added to: tokens and rows without routed pairs keep every bit, signs of
+    zeros among them."""
+    E = 4
+    ids = draw_ids(T, k, E, 51, 0.4)
+    rt = route(ace, ids, E)
+    dy, W = gen(52, T * k, d, dtype=dtype), gen(53, E, d, d, dtype=dtype)
+    ok = L.routed(ids, E)
+    for shared, lost in ((True, ~ok.any(1)), (False, ~ok.reshape(-1))):
+        assert lost.any()
+        dx = torch.full((T if shared else T * k, d), -0.0, dtype=DT[dtype], device="cuda")
+        mode = ace.ACE_INPUT_SHARED if shared else ace.ACE_INPUT_PER_PAIR
+        ace.ace_moe_dx(dy, W, rt, dx, input_mode=mode, accumulate=True)
+        left = dx[torch.from_numpy(lost).cuda()]
+        assert bool((left == 0).all()) and bool(torch.signbit(left).all())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
