@@ -18,6 +18,9 @@
 // as many blocks of a second set (launched behind the first) take.  With splits,
 // that many blocks share a tile's contraction (a tile below is then one of these
 // parts) and store fp32 sums for moe_dx_join_kernel.
+// 8192 x 8192 with a contraction of 1024 131 us, of 2048 228 us (the library's dense
+// products of these sizes 129 and 220): 1.44 us a stage on a full card, whose
+// matrix units bound it, and 6 us a tile for its results.
 
 // Chunk swizzle of a 128-byte W^T row: pairs of chunks trade places, so that the
 // 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread

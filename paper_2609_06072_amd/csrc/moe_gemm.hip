@@ -26,6 +26,9 @@
 // round-robin; block b takes tile (b % 8) * ceil(n_tiles / 8) + b / 8, so each
 // XCD walks a contiguous run of tiles (expert-major): an expert's weight
 // slices stay in one L2.
+//
+// The projection's input gradient (dx = W_e^T dy) has kernels of its own in
+// moe_dx.hpp; their launches and the rule between them are at the end of this file.
 #include <algorithm>
 #include <type_traits>
 
@@ -1008,11 +1011,11 @@ DxPlan dx_plan_bf16(const MoeArgs& a, long P, bool may_split) {
 }
 
 // fp32: streaming with 16, 32 and 64 rows (64 columns), tiles, us a call:
-//   1024, 512, 8            64    18 /  17 /  24 /  89
-//   2048, 1024, 64           4    92 / 101 / 160 / 297      16   133 / 105 / 157 / 298
-//                           64   359 / 263 / 267 / 298     200   865 / 620 / 584 / 572
-//   1024, 2048, 16         128   139 / 115 / 119 / 152     600   562 / 435 / 392 / 419
-//                         1200  1099 / 836 / 757 / 696
+//   1024, 512, 8            64    18 /  19 /  27 /  87
+//   2048, 1024, 64           4    90 / 122 / 184 / 330      16   131 / 111 / 162 / 290
+//                           64   358 / 241 / 244 / 294     200   863 / 580 / 578 / 564
+//   1024, 2048, 16         128   143 / 106 / 107 / 149     600   556 / 419 / 405 / 353
+//                         1200  1091 / 812 / 775 / 687     (uneven routing: 404 / 416)
 // From 128 rows on by rounds of tiles: a CU works through its tiles at the rate of
 // its matrix units, 10% faster per element than the streaming kernel, whose small
 // blocks even out.  Both count half a tile lost per expert.
