@@ -20,7 +20,7 @@
 // parts) and store fp32 sums for moe_dx_join_kernel.
 // 8192 x 8192 with a contraction of 1024 131 us, of 2048 228 us (the library's dense
 // products of these sizes 129 and 220): 1.44 us a stage on a full card, whose
-// matrix units bound it, and 6 us a tile for its results.
+// matrix units bound it, and 8 us a tile for its results and the next one's start.
 
 // Chunk swizzle of a 128-byte W^T row: pairs of chunks trade places, so that the
 // 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread
@@ -588,11 +588,30 @@ __global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
   const uint32_t t = a.per_row.div(idx), col = 4 * (idx - t * a.per_row.d);
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   bool routed = false;
-  for (int j = 0; j < a.k; ++j) {
-    const size_t p = (size_t)t * a.k + j;
-    if (a.pair_row[p] < 0) continue;
-    routed = true;
-    for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(a.part + ((size_t)s * a.pairs + p) * a.d + col);
+  // the loads of eight sums under way at a time, without branches between them
+  // (one token, 8 experts of 2048 x 1024: the call 16.3 -> 13.0 us)
+  constexpr int G = 8;
+  const int n = a.k * a.splits;
+  for (int i0 = 0, j = 0, s = 0; i0 < n; i0 += G) {
+    int row[G];
+    f32x4 f[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const size_t p = (size_t)t * a.k + j;
+      row[g] = a.pair_row[p];
+      f[g] = *reinterpret_cast<const f32x4*>(a.part + ((size_t)s * a.pairs + p) * a.d + col);
+      if (i0 + g + 1 < n && ++s == a.splits) {
+        s = 0;
+        ++j;
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      asm volatile("" : "+v"(f[g]));   // loaded above, not behind the branch
+      if (i0 + g >= n || row[g] < 0) continue;
+      routed = true;
+      v += f[g];
+    }
   }
   if (!routed && (a.keep || a.accumulate)) return;   // (a sum with 0 would lose a zero's sign)
   T4* out = reinterpret_cast<T4*>(static_cast<T*>(a.out) + (size_t)t * a.d + col);
