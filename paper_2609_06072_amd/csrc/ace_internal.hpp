@@ -138,7 +138,10 @@ struct DxPlan {
 };
 // At most so many for a result of `elems` elements.
 constexpr long dx_max_splits(long elems) { return elems <= 1L << 19 ? 8 : elems <= 1L << 22 ? 4 : 1; }
-DxPlan moe_dx_plan(int dtype, const MoeArgs& a, long P, bool may_split);
+// Whether blocks may share a contraction (kDxSummed: a sum over slots, which the
+// join takes the place of, would follow anyway).
+enum DxSums { kDxOnePiece, kDxJoined, kDxSummed };
+DxPlan moe_dx_plan(int dtype, const MoeArgs& a, long P, DxSums sums);
 hipError_t launch_moe_dx(int dtype, DxPlan plan, const MoeArgs& a, long P, hipStream_t stream);
 struct DxJoinArgs {
   const float* part;          // [splits][pairs][d]

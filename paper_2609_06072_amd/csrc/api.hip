@@ -358,12 +358,13 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   a.per_pair = 1;
   const long P = (long)T * k;
   a.pairs = P;
-  const DxPlan plan = moe_dx_plan(dtype, a, P, ws != nullptr);
-  a.splits = plan.splits;
-  a.part = static_cast<float*>(ws);
   // one pair per token: its row is the token's
   const bool rows_are_tokens = im == ACE_INPUT_SHARED && k == 1 && !accumulate;
-  a.y = pair_rows && !rows_are_tokens ? ws : dx;
+  const bool summed = pair_rows && !rows_are_tokens;
+  const DxPlan plan = moe_dx_plan(dtype, a, P, !ws ? kDxOnePiece : summed ? kDxSummed : kDxJoined);
+  a.splits = plan.splits;
+  a.part = static_cast<float*>(ws);
+  a.y = summed ? ws : dx;
   hipError_t e = launch_moe_dx(dtype, plan, a, P, st);
   if (e == hipSuccess && a.splits > 1) {
     DxJoinArgs j{};

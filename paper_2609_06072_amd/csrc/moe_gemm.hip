@@ -30,6 +30,7 @@
 // The projection's input gradient (dx = W_e^T dy) has kernels of its own in
 // moe_dx.hpp; their launches and the rule between them are at the end of this file.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "ace_device.hpp"
@@ -915,11 +916,13 @@ bool mid_f32(const MoeArgs& a, long P) {
 namespace {
 
 // The input gradient: which kernel.  The number of tiles of bm x bn is estimated
-// from the average number of rows per expert (half a tile lost in each that can be
-// hit; the host does not know the routing), one for each of these at least.
+// from the average number of rows per expert (half a tile lost in each that an even
+// routing would hit; the host does not know the routing), one for each of these at
+// least.
 
 long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
-  const long hit = P < a.E ? P : a.E, rows = P / bm + hit / 2;
+  const double missed = std::pow(1. - std::min(1., (double)a.k / a.E), (double)(P / a.k));
+  const long hit = std::max(1L, std::lround(a.E * (1. - missed))), rows = P / bm + hit / 2;
   return (rows > hit ? rows : hit) * ((a.d_out + bn - 1) / bn);
 }
 
@@ -964,29 +967,31 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 constexpr long kDxStream32 = 20, kDxShortK = 640, kDxShort32 = 80;
 
 // Blocks per tile of the narrow forms: as many as fill the chip once (fp32, whose
-// matrix work is longer: twice), each with 640 (fp32: 320) of the contraction at
-// least; the join takes the place of the sum over slots, or 2 us more per pair.
+// matrix work is longer: twice), each with 320 of the contraction at least, in bf16
+// 640 where the join does not take the place of the sum over slots (460 pairs of 496
+// x 608, 4 experts: 10.1 us a call, in two 12.2).
 // us a call, shared input (1 / 2 / 4 / 8 blocks a tile):
-//   bf16  9816 x 544, 4 experts, 16 pairs      47.1 / 29.1 / 20.6 / 21.1
-//         2000 x 304, 8, 240                   21.2 / 16.1 / 15.6 / 19.4
-//         1504 x 1000, 8, 80                   16.5 / 14.1 / 15.1 / 18.8
-//         1024 x 512, 8, 512                   11.3 / 11.6 / 12.6 / 18.8
-//   fp32  4952 x 296, 64, 6                    50.9 / 29.9 / 20.1 / 16.1
-//         1568 x 424, 4, 200                   27.7 / 18.8 / 15.1 / 18.1
-//         1024 x 512, 8, 512                   20.4 / 19.6 / 18.7 / 23.4 (3: 17.3)
-//         1012 x 1924, 4, 132                  22.2 / 22.7 / 27.2 / 34.6
-DxPlan dx_narrow(bool f32, DxKernel kernel, const MoeArgs& a, long P, bool may_split) {
+//   bf16  9816 x 544, 4 experts, 16 pairs      46.6 / 28.1 / 18.8 / 18.6
+//         2000 x 304, 8, 240                   18.7 / 13.6 / 11.0 / 11.8
+//         1504 x 1000, 8, 80                   15.3 / 13.4 / 13.6 / 16.5
+//         1024 x 512, 8, 512                   10.8 / 11.6 / 12.3 / 17.4
+//   fp32  4952 x 296, 64, 6                    50.5 / 29.3 / 18.5 / 13.4
+//         1568 x 424, 4, 200                   28.0 / 18.7 / 13.9 / 16.0
+//         1024 x 512, 8, 512                   20.9 / 19.9 / 18.5 / 20.9
+//         1016 x 1920, 4, 132                  20.5 / 20.1 / 18.4 / 24.1
+DxPlan dx_narrow(bool f32, DxKernel kernel, const MoeArgs& a, long P, DxSums sums) {
   const long bm = kernel == kDxS16x64 ? 16 : kernel == kDxS32x64 ? 32 : 64;
-  const long fill = (f32 ? 2L : 1L) * device_cu_count() / dx_blocks(a, P, bm, 64), most = a.d_in / (f32 ? 320 : 640);
-  return {kernel, may_split ? (int)std::max(1L, std::min({fill, most, dx_max_splits(P * a.d_out)})) : 1};
+  const long fill = (f32 ? 2L : 1L) * device_cu_count() / dx_blocks(a, P, bm, 64);
+  const long most = a.d_in / (f32 || sums == kDxSummed ? 320 : 640);
+  return {kernel, sums != kDxOnePiece ? (int)std::max(1L, std::min({fill, most, dx_max_splits(P * a.d_out)})) : 1};
 }
 
-DxPlan dx_plan_bf16(const MoeArgs& a, long P, bool may_split) {
+DxPlan dx_plan_bf16(const MoeArgs& a, long P, DxSums sums) {
   const long cus = device_cu_count(), K = a.d_in;
   const long tiles = dx_blocks(a, P, Large::BM, Large::BN);
   long large = -1;   // ns, without the call's 5
   int splits = 1;
-  for (int s = 1; s <= (may_split ? dx_max_splits(P * a.d_out) : 1) && K / s >= kDxLargeK; ++s) {
+  for (int s = 1; s <= (sums != kDxOnePiece ? dx_max_splits(P * a.d_out) : 1) && K / s >= kDxLargeK; ++s) {
     const long over = tiles * s % cus, Ks = K / s;
     const long round = 8000 + 29 * Ks;
     const long last = over == 0 ? 0 : 4 * over <= cus ? 6000 + 16 * Ks : 2 * over <= cus ? 6000 + 19 * Ks : round;
@@ -1001,7 +1006,7 @@ DxPlan dx_plan_bf16(const MoeArgs& a, long P, bool may_split) {
   const long blocks = dx_blocks(a, P, 64, 64);
   const bool fit32 = dx_blocks(a, P, 32, 64) <= cus;
   if (fit32 || blocks <= cus) {
-    stream = dx_narrow(false, fit32 ? kDxS32x64 : kDxS64x64, a, P, may_split);
+    stream = dx_narrow(false, fit32 ? kDxS32x64 : kDxS64x64, a, P, sums);
     t = -1000 + (fit32 ? 9 : 12) * K / 2 / stream.splits + (stream.splits > 1 ? 3000 : 0);
   } else if (K <= kDxShortK && P > kDxStream32 * a.E) {
     stream = {P <= kDxShort32 * a.E ? kDxS32x64 : kDxS64x64, 1};
@@ -1021,19 +1026,19 @@ DxPlan dx_plan_bf16(const MoeArgs& a, long P, bool may_split) {
 // blocks even out.  Both count half a tile lost per expert.
 constexpr long kDxStream16F32 = 8, kDxStream32F32 = 128;
 
-DxPlan dx_plan_f32(const MoeArgs& a, long P, bool may_split) {
-  if (P <= kDxStream16F32 * a.E) return dx_narrow(true, kDxS16x64, a, P, may_split);
-  if (P <= kDxStream32F32 * a.E) return dx_narrow(true, kDxS32x64, a, P, may_split);
+DxPlan dx_plan_f32(const MoeArgs& a, long P, DxSums sums) {
+  if (P <= kDxStream16F32 * a.E) return dx_narrow(true, kDxS16x64, a, P, sums);
+  if (P <= kDxStream32F32 * a.E) return dx_narrow(true, kDxS32x64, a, P, sums);
   const long cus = device_cu_count(), BM = DxTile::BM, BN = DxTile::BN;
   const long tiles = (P / BM + a.E / 2) * ((a.d_out + BN - 1) / BN);
   const bool ahead = 9 * ((tiles + cus - 1) / cus * cus) * BM * BN < 10 * (P + 32 * (long)a.E) * a.d_out;
-  return ahead ? DxPlan{kDxTiles, 1} : dx_narrow(true, kDxS64x64, a, P, may_split);
+  return ahead ? DxPlan{kDxTiles, 1} : dx_narrow(true, kDxS64x64, a, P, sums);
 }
 
 }  // namespace
 
-DxPlan moe_dx_plan(int dtype, const MoeArgs& a, long P, bool may_split) {
-  return dtype == ACE_F32 ? dx_plan_f32(a, P, may_split) : dx_plan_bf16(a, P, may_split);
+DxPlan moe_dx_plan(int dtype, const MoeArgs& a, long P, DxSums sums) {
+  return dtype == ACE_F32 ? dx_plan_f32(a, P, sums) : dx_plan_bf16(a, P, sums);
 }
 
 hipError_t launch_moe_dx(int dtype, DxPlan plan, const MoeArgs& a, long P, hipStream_t stream) {
