@@ -75,6 +75,22 @@ __device__ inline u32x2 round4(f32x4 v) {
   return __builtin_bit_cast(u32x2, bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]});
 }
 
+// Columns 4 g .. 4 g + 3 of a row's two neighbouring 16-column blocks (lane (c16,
+// g)) as bf16: the lanes of a row trade their 8-byte pieces until lane g holds the 16
+// bytes 8 g .. 8 g + 7 of the 32 columns.
+__device__ inline u32x4 trade4(f32x4 a, f32x4 b) {
+  const u32x2 lo = round4(a), hi = round4(b);
+  u32x4 o;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    u32x2 s = __builtin_amdgcn_permlane32_swap(lo[i], hi[i], false, false);
+    s = __builtin_amdgcn_permlane16_swap(s[0], s[1], false, false);
+    o[i] = s[0];
+    o[2 + i] = s[1];
+  }
+  return o;
+}
+
 // The lane's number, computed where it is asked for.
 __device__ inline int lane_id() {
   int l;
@@ -342,16 +358,7 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
       for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+a"(acc[nb][mb]));   // read behind mfma_done
       u32x4 o[NB / 2];
 #pragma unroll
-      for (int nb = 0; nb < NB; nb += 2) {
-        u32x2 lo = round4(acc[nb][mb]), hi = round4(acc[nb + 1][mb]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          u32x2 s = __builtin_amdgcn_permlane32_swap(lo[i], hi[i], false, false);
-          s = __builtin_amdgcn_permlane16_swap(s[0], s[1], false, false);
-          o[nb / 2][i] = s[0];
-          o[nb / 2][2 + i] = s[1];
-        }
-      }
+      for (int nb = 0; nb < NB; nb += 2) o[nb / 2] = trade4(acc[nb][mb], acc[nb + 1][mb]);
       const int p = __shfl(pc[mb >> 2], 16 * (mb & 3) + lc16, 64);
       if (!FULL && a.splits > 1) {
         if (row0 + 16 * mb < cur.hi) {
@@ -622,58 +629,67 @@ __global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
   *out = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
 }
 
-// ---- fp32, many rows per expert: tiles of 128 rows x 128 columns, four waves of
-// 64 x 64, K-blocks of 16 in a ring of three in LDS (48 KB, three blocks per CU:
-// while one waits or stores, the others use the matrix units, which bound the
-// call).  Tile order as in the large bf16 tiles.
+// ---- tiles of 128 rows x 128 columns, four waves of 64 x 64, one K-block a stage
+// in a ring in LDS, several blocks per CU (while one waits or stores, the others use
+// the matrix units): fp32 with many rows per expert, bf16 where the large tiles leave
+// CUs idle.  Tile order as in the large tiles; with splits, that many blocks share a
+// tile's K-blocks and store fp32 sums for moe_dx_join_kernel.
+template <typename T>
 struct DxTile {
-  static constexpr int KB = 16, BM = 128, BN = 128, NBUF = 3;
-  static constexpr int XBYTES = BM * kGRowBytes, STAGE = XBYTES + KB * BN * 4, COPIES = 2;
+  static constexpr int KB = Tr<T>::KB, BM = 128, BN = 128, NBUF = sizeof(T) == 4 ? 3 : 4, PER_CU = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int XBYTES = BM * kGRowBytes, STAGE = XBYTES + KB * BN * (int)sizeof(T), COPIES = 2;
+  static constexpr int WCH = BN * (int)sizeof(T) / 16, RPC = 64 / WCH;   // chunks of a W row, rows of a copy
 };
 
-__global__ __launch_bounds__(256, 3) void moe_dx_tile_kernel(MoeArgs a) {
-  using C = DxTile;
-  using F = f32x4;
+template <typename T>
+__global__ __launch_bounds__(256, DxTile<T>::PER_CU) void moe_dx_tile_kernel(MoeArgs a) {
+  using C = DxTile<T>;
+  using F = typename Tr<T>::frag;
+  constexpr int PER = Tr<T>::PER;
   __shared__ __attribute__((aligned(16))) char smem[C::NBUF * C::STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, g = lane >> 4;
   const int wy = wave >> 1, wx = wave & 1;
-  const int n_tiles = count_tiles(a.offsets, a.E, C::BM) * a.nt;
-  const int per_xcd = (n_tiles + kXcds - 1) / kXcds;
+  const int n_items = count_tiles(a.offsets, a.E, C::BM) * a.nt * a.splits;
+  const int per_xcd = (n_items + kXcds - 1) / kXcds;
   const int bi = blockIdx.x / kXcds;
-  const int tile = (blockIdx.x % kXcds) * per_xcd + bi;
-  if (bi >= per_xcd || tile >= n_tiles) return;
+  const int item = (blockIdx.x % kXcds) * per_xcd + bi;
+  if (bi >= per_xcd || item >= n_items) return;
   int e, lo, hi, rem;
-  if (!locate_key(a.offsets, a.E, C::BM, a.nt, tile, &e, &lo, &hi, &rem)) return;
+  if (!locate_key(a.offsets, a.E, C::BM, a.nt, item / a.splits, &e, &lo, &hi, &rem)) return;
+  const int split = item % a.splits;
   const int m_e = (hi - lo + C::BM - 1) / C::BM;
   const int grp = rem / (kRowGroup * a.nt), gsz = min(kRowGroup, m_e - grp * kRowGroup);
   const int ing = rem - grp * kRowGroup * a.nt;
   const int n0 = ing / gsz * C::BN;
   const int u0 = lo + (grp * kRowGroup + ing % gsz) * C::BM;
   const int K = a.d_in, N = a.d_out;
-  const float* X = static_cast<const float*>(a.x);
-  const float* Wt = static_cast<const float*>(a.W) + (size_t)e * K * N + n0;
-  // copies of wave w: x rows 32 w + 16 i + (lane >> 2), W rows 4 w + 2 i + (lane >> 5)
-  const float* xsrc[C::COPIES];
+  const T* X = static_cast<const T*>(a.x);
+  const T* Wt = static_cast<const T*>(a.W) + (size_t)e * K * N + n0;
+  // copies of wave w: x rows 32 w + 16 i + (lane >> 2), W rows RPC (2 w + i) + lane / WCH
+  const int wrow = C::RPC * 2 * wave + lane / C::WCH;
+  const T* xsrc[C::COPIES];
   int wcol[C::COPIES];
 #pragma unroll
   for (int i = 0; i < C::COPIES; ++i) {
     xsrc[i] = X + (size_t)a.pair_list[min(u0 + 32 * wave + 16 * i + (lane >> 2), hi - 1)] * K;
-    wcol[i] = min(4 * ((lane & 31) ^ wt_swz<float, C::BN>(4 * wave + 2 * i + (lane >> 5))), N - 4 - n0);
+    wcol[i] = min(PER * ((lane % C::WCH) ^ wt_swz<T, C::BN>(wrow + C::RPC * i)), N - PER - n0);
   }
-  const int xcol = 4 * ((lane & 3) ^ g_swz(lane >> 2));
-  const int nst = (K + C::KB - 1) / C::KB;
+  const int xcol = PER * ((lane & 3) ^ g_swz(lane >> 2));
+  // K-blocks st0 .. st0 + nst - 1
+  const int all = (K + C::KB - 1) / C::KB, share = (all + a.splits - 1) / a.splits;
+  const int st0 = split * share, nst = max(0, min(share, all - st0));
   const uint32_t sbase = lds_addr(smem);
   auto issue = [&](int st) {
     const uint32_t buf = sbase + (st % C::NBUF) * C::STAGE;
-    const int k0 = st * C::KB;
-    const float* Wk = Wt + (size_t)k0 * N;
+    const int k0 = (st0 + st) * C::KB;
+    const T* Wk = Wt + (size_t)k0 * N;
 #pragma unroll
     for (int i = 0; i < C::COPIES; ++i) {
-      dma16(xsrc[i] + min(k0 + xcol, K - 4), __builtin_amdgcn_readfirstlane(buf + (32 * wave + 16 * i) * kGRowBytes));
-      const int row = min(4 * wave + 2 * i + (lane >> 5), K - 1 - k0);
+      dma16(xsrc[i] + min(k0 + xcol, K - PER), __builtin_amdgcn_readfirstlane(buf + (32 * wave + 16 * i) * kGRowBytes));
+      const int row = min(wrow + C::RPC * i, K - 1 - k0);
       dma16(Wk + ((uint32_t)row * (uint32_t)N + (uint32_t)wcol[i]),
-            __builtin_amdgcn_readfirstlane(buf + C::XBYTES + (4 * wave + 2 * i) * C::BN * 4));
+            __builtin_amdgcn_readfirstlane(buf + C::XBYTES + (2 * wave + i) * 1024));
     }
   };
   f32x4 acc[4][4];
@@ -689,32 +705,46 @@ __global__ __launch_bounds__(256, 3) void moe_dx_tile_kernel(MoeArgs a) {
     __syncthreads();
     if (st + C::NBUF - 1 < nst) issue(st + C::NBUF - 1);
     const char* S = smem + (st % C::NBUF) * C::STAGE;
-    const bool past = st * C::KB + 4 * g >= K;
+    const bool past = (st0 + st) * C::KB + PER * g >= K;
     F xf[4], wf[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       xf[i] = *reinterpret_cast<const F*>(S + (64 * wy + 16 * i + c16) * kGRowBytes + ((g ^ g_swz(c16)) << 4));
-      wf[i] = wt_frag<float, C::BN>(S + C::XBYTES, 64 * wx + 16 * i, lane);
-      if (past) xf[i] = wf[i] = Tr<float>::zero();
+      wf[i] = wt_frag<T, C::BN>(S + C::XBYTES, 64 * wx + 16 * i, lane);
+      if (past) xf[i] = wf[i] = Tr<T>::zero();
     }
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)   // the four products of an accumulator block apart
+      for (int i = 0; i < 4; ++i)   // the four products of an accumulator block apart
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+          for (int mb = 0; mb < 4; ++mb)   // D[column][row]
+            acc[nb][mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[nb][i], xf[mb][i], acc[nb][mb], 0, 0, 0);
+    } else {
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb)
 #pragma unroll
-        for (int mb = 0; mb < 4; ++mb)   // D[column][row]
-          acc[nb][mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[nb][i], xf[mb][i], acc[nb][mb], 0, 0, 0);
+        for (int mb = 0; mb < 4; ++mb) acc[nb][mb] = Tr<T>::mma(wf[nb], xf[mb], acc[nb][mb]);
+    }
   }
-  float* Y = static_cast<float*>(a.y);
-  const int col0 = n0 + 64 * wx + 4 * g;
+  T* Y = static_cast<T*>(a.y);
+  const int col0 = n0 + 64 * wx + 4 * g, col8 = n0 + 64 * wx + 8 * g;
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) {
     const int u = u0 + 64 * wy + 16 * mb + c16;
-    if (u < hi) {
-      float* row = Y + (size_t)a.pair_list[u] * N + col0;
+    const size_t at = (size_t)a.pair_list[min(u, hi - 1)] * N;
+    if (sizeof(T) == 4 || a.splits > 1) {
+      float* row = (a.splits > 1 ? a.part + (size_t)split * a.pairs * N : reinterpret_cast<float*>(Y)) + at + col0;
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb)
-        if (col0 + 16 * nb < N) *reinterpret_cast<f32x4*>(row + 16 * nb) = acc[nb][mb];
+        if (u < hi && col0 + 16 * nb < N) *reinterpret_cast<f32x4*>(row + 16 * nb) = acc[nb][mb];
+    } else {
+#pragma unroll
+      for (int nb = 0; nb < 4; nb += 2) {   // (before the branch: lanes trade pieces)
+        const u32x4 o = trade4(acc[nb][mb], acc[nb + 1][mb]);
+        if (u < hi && col8 + 16 * nb < N) *reinterpret_cast<u32x4*>(Y + at + col8 + 16 * nb) = o;
+      }
     }
   }
 }

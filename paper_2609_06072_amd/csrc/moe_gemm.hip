@@ -836,13 +836,14 @@ hipError_t launch_moe_dx_stream(MoeArgs a, long P, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <typename T>
 hipError_t launch_moe_dx_tile(MoeArgs a, long P, hipStream_t stream) {
-  using C = DxTile;
+  using C = DxTile<T>;
   a.nt = (a.d_out + C::BN - 1) / C::BN;
-  const long max_tiles = ((P + C::BM - 1) / C::BM + a.E) * a.nt;
+  const long max_tiles = ((P + C::BM - 1) / C::BM + a.E) * a.nt * a.splits;
   const long grid = (max_tiles + kXcds - 1) / kXcds * kXcds;
   if (grid > 0x7fffffffL) return hipErrorInvalidConfiguration;
-  moe_dx_tile_kernel<<<(int)grid, 256, 0, stream>>>(a);
+  moe_dx_tile_kernel<T><<<(int)grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -932,6 +933,8 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //                6 + 16 K in quarters
 //   streaming, 64 rows x 128 columns (one block per CU)   4 + 9.5 K a round
 //   64 x 64, two blocks per CU, for short contractions    2.3 + 3 K per CU's block
+//   128 x 128, two blocks per CU   0.4 + 16 K per CU's tile, at least one, half way
+//                from the tiles' number over the CUs' to the next whole number
 //   32 x 64 and 64 x 64 where they fit the CUs once       4 + 4.5 K and 4 + 6 K in all
 // and where blocks share a contraction 3 more (large tiles: also their sums at 5
 // TB/s), decide between large tiles and streaming.  us a call, measured 64 x 128 /
@@ -946,6 +949,12 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //   5032, 456, 16           200    79 /  93       444   137 /  99
 //   1568, 424, 4            981    23 /  32      2000    42 /  35
 //   512, 256, 8             500    10 /  12      1000    16 /  13
+// Best of the above / 128 x 128 (in one, or * two blocks a contraction):
+//   1440, 1504, 4           578    42 /  32         3456, 272, 16    1104    87 /  74
+//   1032, 1320, 8           322    32 /  25         2200, 288, 32     595    69 /  60
+//   2048, 1024, 64           64    74 /  65         2336, 1544, 8      75    34 /  27 *
+//   4096, 4096, 8            64    77 /  65          264, 496, 96      75    22 /  17
+//   1024, 2048, 64          512   192 / 258          616, 1560, 128   214   128 / 162
 // Large tiles, one block for a contraction / as many as estimated best:
 //   7784, 912, 16           164   178 / 121
 //   6728, 568, 32           147   151 / 125
@@ -1012,7 +1021,23 @@ DxPlan dx_plan_bf16(const MoeArgs& a, long P, DxSums sums) {
     stream = {P <= kDxShort32 * a.E ? kDxS32x64 : kDxS64x64, 1};
     t = blocks * (2300 + 3 * K) / cus;
   }
-  return large >= 0 && P > kDxStream32 * a.E && large < t ? DxPlan{kDxLarge, splits} : stream;
+  if (P <= kDxStream32 * a.E) return stream;
+  DxPlan best = stream;
+  if (large >= 0 && large < t) {
+    best = {kDxLarge, splits};
+    t = large;
+  }
+  const long mid = dx_blocks(a, P, DxTile<__bf16>::BM, DxTile<__bf16>::BN);
+  for (int s = 1; s <= (sums != kDxOnePiece ? dx_max_splits(P * a.d_out) : 1) && (s == 1 || K / s >= 320); ++s) {
+    const long rounds = (mid * s + cus - 1) / cus;
+    const long tm = (std::max(mid * s, cus) + rounds * cus) * (190 + 8 * K / s) / cus +
+                    (s > 1 ? 3000 + s * P * a.d_out * 8 / 5000 : 0);
+    if (tm < t) {
+      best = {kDxTiles, s};
+      t = tm;
+    }
+  }
+  return best;
 }
 
 // fp32: streaming with 16, 32 and 64 rows (64 columns), tiles, us a call:
@@ -1029,7 +1054,7 @@ constexpr long kDxStream16F32 = 8, kDxStream32F32 = 128;
 DxPlan dx_plan_f32(const MoeArgs& a, long P, DxSums sums) {
   if (P <= kDxStream16F32 * a.E) return dx_narrow(true, kDxS16x64, a, P, sums);
   if (P <= kDxStream32F32 * a.E) return dx_narrow(true, kDxS32x64, a, P, sums);
-  const long cus = device_cu_count(), BM = DxTile::BM, BN = DxTile::BN;
+  const long cus = device_cu_count(), BM = DxTile<float>::BM, BN = DxTile<float>::BN;
   const long tiles = (P / BM + a.E / 2) * ((a.d_out + BN - 1) / BN);
   const bool ahead = 9 * ((tiles + cus - 1) / cus * cus) * BM * BN < 10 * (P + 32 * (long)a.E) * a.d_out;
   return ahead ? DxPlan{kDxTiles, 1} : dx_narrow(true, kDxS64x64, a, P, sums);
@@ -1049,7 +1074,7 @@ hipError_t launch_moe_dx(int dtype, DxPlan plan, const MoeArgs& a, long P, hipSt
     if (k == kDxS32x64 && !runs32) return launch_moe_dx_stream<float, 2, 64, false>(a, P, stream);
     if (k == kDxS32x64) return launch_moe_dx_stream<float, 2, 64, true>(a, P, stream);
     if (k == kDxS64x64) return launch_moe_dx_stream<float, 4, 64, true>(a, P, stream);
-    return launch_moe_dx_tile(a, P, stream);
+    return launch_moe_dx_tile<float>(a, P, stream);
   }
   if (k == kDxS32x64 && !runs32) return launch_moe_dx_stream<__bf16, 2, 64, false>(a, P, stream);
   if (k == kDxS32x64) return launch_moe_dx_stream<__bf16, 2, 64, true>(a, P, stream);
@@ -1058,6 +1083,7 @@ hipError_t launch_moe_dx(int dtype, DxPlan plan, const MoeArgs& a, long P, hipSt
   if (k == kDxS32x128) return launch_moe_dx_stream<__bf16, 2, 128, false>(a, P, stream);
   if (k == kDxS64x128 && !runs64) return launch_moe_dx_stream<__bf16, 4, 128, false>(a, P, stream);
   if (k == kDxS64x128) return launch_moe_dx_stream<__bf16, 4, 128, true>(a, P, stream);
+  if (k == kDxTiles) return launch_moe_dx_tile<__bf16>(a, P, stream);
   return launch_moe_dx_large(a, P, stream);
 }
 

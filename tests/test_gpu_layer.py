@@ -101,10 +101,10 @@ DX_SIZES = [
     (90, 2, 256, 64, 64, 0.0, 0.0),         # the most experts
     (2, 2, 8, 544, 4104, 0.0, 0.0),         # few tiles: several blocks a contraction
     (40, 3, 4, 72, 2056, 0.2, 0.0),
-    (1300, 2, 8, 264, 328, 0.02, 0.8),      # a ragged contraction in large tiles
+    (1300, 2, 8, 264, 328, 0.02, 0.8),
     (700, 2, 2, 1096, 384, 0.0, 0.0),
-    (2600, 2, 2, 1032, 264, 0.0, 0.0),      # 110 large tiles: in halves
-    (4000, 2, 2, 2056, 256, 0.0, 0.0),      # 288: a round, then quarters
+    (2600, 2, 2, 1032, 264, 0.0, 0.0),
+    (4000, 2, 2, 2056, 256, 0.0, 0.0),
     (320, 2, 64, 320, 72, 0.0, 0.0),        # the streaming forms: 32 x 128,
     (1000, 2, 64, 328, 136, 0.0, 0.8),      # 64 x 128,
     (1000, 2, 4, 520, 136, 0.05, 0.0),      # with several row tiles per expert,
@@ -112,13 +112,19 @@ DX_SIZES = [
     (800, 2, 8, 328, 136, 0.0, 0.8),        # with several row tiles
     (1030, 2, 2, 1920, 72, 0.0, 0.0),       # fp32 tiles
     (1500, 1, 3, 520, 264, 0.1, 0.0),       # one pair per token, some dropped
-    (600, 2, 2, 264, 2056, 0.05, 0.0),      # large tiles that share contractions,
-    (600, 2, 2, 264, 2048, 0.05, 0.0),      # whole stages each,
-    (2500, 1, 1, 1000, 4200, 0.0, 0.0),     # in parts and several a block
-    (3000, 2, 16, 264, 1536, 0.0, 0.8),     # large tiles, two blocks a contraction,
-    (3000, 2, 16, 264, 1544, 0.05, 0.0),    # ragged
-    (3000, 4, 200, 256, 1024, 0.05, 0.8),   # large tiles of many experts
-    (2600, 2, 2, 1024, 256, 0.0, 0.0),      # whole stages, in halves
+    (600, 2, 2, 264, 2056, 0.05, 0.0),
+    (600, 2, 2, 264, 2048, 0.05, 0.0),
+    (2500, 1, 1, 1000, 4200, 0.0, 0.0),     # large tiles that share contractions
+    (3000, 2, 16, 264, 1536, 0.0, 0.8),     # bf16 tiles of 128 x 128,
+    (3000, 2, 16, 264, 1544, 0.05, 0.0),    # ragged,
+    (3000, 4, 200, 256, 1024, 0.05, 0.8),   # many experts,
+    (150, 4, 8, 1544, 2336, 0.05, 0.0),     # two blocks a contraction,
+    (200, 4, 8, 1544, 2312, 0.0, 0.0),      # ragged
+    (2500, 1, 1, 1000, 4224, 0.0, 0.0),     # large tiles, blocks of whole stages,
+    (10000, 4, 200, 256, 512, 0.05, 0.5),   # many experts,
+    (2600, 2, 2, 1024, 768, 0.0, 0.0),      # in halves,
+    (2600, 2, 2, 1032, 776, 0.05, 0.0),     # ragged,
+    (4000, 2, 2, 2056, 640, 0.0, 0.0),      # a round, then quarters
     (1000, 2, 64, 264, 648, 0.0, 0.0),      # 64 x 128 streaming,
     (1200, 2, 32, 504, 648, 0.0, 0.0),      # with several row tiles
 ]
@@ -183,10 +189,11 @@ def test_moe_dx_infinities_stay_in_their_rows(ace, dtype):
         close("finite rows", f64(dx)[keep], ref[keep], tol[keep])
 
 
-def test_moe_dx_infinities_in_large_tiles(ace):
-    """The same where tiles of 256 rows share a ragged contraction: its end is
-    filled with zeros on both sides."""
-    T, k, E, d_in, d_out = 6000, 1, 16, 264, 1544
+@pytest.mark.parametrize("E,d_in,d_out", [(16, 264, 1544), (4, 1032, 776)])
+def test_moe_dx_infinities_in_large_tiles(ace, E, d_in, d_out):
+    """The same in tiles of 128 and of 256 rows with a ragged contraction: its end
+    is filled with zeros on both sides."""
+    T, k = 6000, 1
     ids = (np.arange(T, dtype=np.int32) % E).reshape(T, 1)
     rt = route(ace, ids, E)
     dy, W = gen(6, T, d_out), gen(7, E, d_out, d_in)
