@@ -271,8 +271,7 @@ def ace_group_permute_noalloc(topk_ids: torch.Tensor, E: int,
     routing.check_capacity(T, k, n_keys)
     _check(_lib.ace_group_permute_noalloc(_ptr(topk_ids), T, k, E, _ptr(expert_to_group), G,
                                           mode, ctypes.byref(routing.c), _stream(stream)),
-           "ace_group_permute_noalloc", "ace_moe_dx", "ace_moe_combine_fwd", "ace_moe_combine_bwd",
-           "ace_act_pack", "ace_act_unpack", "ace_swiglu_fwd", "ace_swiglu_bwd")
+           "ace_group_permute_noalloc")
     return routing
 
 
