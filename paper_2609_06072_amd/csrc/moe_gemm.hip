@@ -936,9 +936,10 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //   128 x 128, two blocks per CU   0.4 + 16 K per CU's tile, at least one, half way
 //                from the tiles' number over the CUs' to the next whole number
 //   32 x 64 and 64 x 64 where they fit the CUs once       4 + 4.5 K and 4 + 6 K in all
-// and where blocks share a contraction 3 more (large tiles: also their sums at 5
-// TB/s), decide between large tiles and streaming.  us a call, measured 64 x 128 /
-// large, random routings, weights out of every cache, contractions not shared:
+// and where blocks share a contraction 3 more (tiles: also their sums at 5 TB/s).
+// The least decides; up to 20 rows per expert it is streaming.  us a call, measured
+// 64 x 128 / large, random routings, weights out of every cache, contractions not
+// shared:
 //   K, columns, experts     rows per expert
 //   2048, 1024, 64           32    58 /  70        64    87 /  69      100   117 /  71
 //   4096, 4096, 8            32    53 /  76        64    91 /  74      128   128 /  93
