@@ -19,8 +19,9 @@
 // that many blocks share a tile's contraction (a tile below is then one of these
 // parts) and store fp32 sums for moe_dx_join_kernel.
 // 8192 x 8192 with a contraction of 1024 131 us, of 2048 228 us (the library's dense
-// products of these sizes 129 and 220): 1.44 us a stage on a full card, whose
-// matrix units bound it, and 8 us a tile for its results and the next one's start.
+// products of these sizes 129 and 220): 1.44 us a stage on a full card, 1.24 for a
+// block alone, of which the matrix units are busy for 0.9, and 8 us a tile for its
+// results and the next one's start.
 
 // Chunk swizzle of a 128-byte W^T row: pairs of chunks trade places, so that the
 // 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread
