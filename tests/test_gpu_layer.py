@@ -95,7 +95,7 @@ DX_SIZES = [
     (130, 4, 7, 264, 136, 0.1, 0.8),
     (200, 8, 16, 1000, 264, 0.0, 0.8),
     (300, 2, 3, 520, 328, 0.05, 1.0),
-    (1030, 2, 4, 512, 256, 0.0, 0.0),       # several large tiles of an expert
+    (1030, 2, 4, 512, 256, 0.0, 0.0),       # several row tiles of an expert
     (2100, 1, 2, 264, 136, 0.02, 0.0),
     (257, 32, 40, 64, 48, 0.3, 0.0),        # the most slots
     (90, 2, 256, 64, 64, 0.0, 0.0),         # the most experts
@@ -106,8 +106,8 @@ DX_SIZES = [
     (2600, 2, 2, 1032, 264, 0.0, 0.0),
     (4000, 2, 2, 2056, 256, 0.0, 0.0),
     (320, 2, 64, 320, 72, 0.0, 0.0),        # the streaming forms: 32 x 128,
-    (1000, 2, 64, 328, 136, 0.0, 0.8),      # 64 x 128,
-    (1000, 2, 4, 520, 136, 0.05, 0.0),      # with several row tiles per expert,
+    (1000, 2, 64, 328, 136, 0.0, 0.8),
+    (1000, 2, 4, 520, 136, 0.05, 0.0),
     (750, 2, 32, 328, 136, 0.0, 0.0),       # 64 x 64,
     (800, 2, 8, 328, 136, 0.0, 0.8),        # with several row tiles
     (1030, 2, 2, 1920, 72, 0.0, 0.0),       # fp32 tiles
