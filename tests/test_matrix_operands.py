@@ -80,5 +80,5 @@ MFMA = "\t;;#ASMSTART\n\tv_mfma_f32_16x16x32_bf16 a[8:11], v[0:3], v[4:7], a[8:1
     ("\tv_add_u32_e32 v4, v8, v9\n\ts_branch .L1\n\ts_nop 5\n.L1:\n", True),
     ("\tv_add_u32_e32 v4, v8, v9\n\ts_nop 5\n.L1:\n", False),
 ])
-def test_checker(before, bad):
+def test_scan_of_planted_hazards(before, bad):
     assert bool(unready(before + MFMA)) == bad
