@@ -329,13 +329,12 @@ ace_status ace_moe_lora_fwd(ace_dtype dtype, ace_input_mode input_mode, int32_t 
  *               was).  Must not overlap dy or W.
  *   ws          device scratch of at least
  *               ace_workspace_bytes(ACE_OP_MOE_DX, T, k, d_in, d_out, E, 0)
- *               where it holds a row of dtype per pair (the products are summed
- *               in fp32 and rounded to dtype there; a token's rows are then
- *               added in fp32, in slot order, and rounded once; with k = 1 the
- *               row is the result), or, in calls of few tiles, fp32 sums over
- *               parts of a contraction that several blocks share.  May be NULL
- *               for the per-pair input with accumulate = 0: then no contraction
- *               is shared.  No initialisation.
+ *               where it holds an fp32 row per pair (a token's rows are added in
+ *               slot order, then to dx where accumulate asks for it, all in fp32,
+ *               and the result is rounded once), in calls of few tiles one for
+ *               each of the blocks that share a contraction.  May be NULL for the
+ *               per-pair input with accumulate = 0: then no contraction is
+ *               shared.  No initialisation.
  * Limits: T * k * d_out and T * k * d_in below 2^33 - 4096, d_in below 2^24,
  * d_out below 2^30.
  * Deterministic.

@@ -113,7 +113,8 @@ struct MoeArgs {
   const int32_t* row_token;
   const uint32_t* row_slots;
   const int32_t* pair_list;   // launch_moe_dx: pair of each row
-  float* part;                // launch_moe_dx: sums of the splits
+  float* part;                // launch_moe_dx: [splits][P][d_out] fp32 sums to be joined, or
+                              // null (y is written; one split)
   long pairs;
   int32_t splits;
   int32_t E, k, d_in, d_out, per_pair;
@@ -133,18 +134,17 @@ hipError_t launch_moe_gemm(int dtype, const MoeArgs& a, long P, hipStream_t stre
 enum DxKernel { kDxS16x64, kDxS32x64, kDxS64x64, kDxS32x128, kDxS64x128, kDxTiles, kDxLarge };
 struct DxPlan {
   DxKernel kernel;
-  int splits;   // blocks that share a tile's contraction (1: a.y is written; otherwise
-                // a.part, [splits][P][d_out] fp32, to be joined)
+  int splits;   // blocks that share a tile's contraction
 };
 // At most so many for a result of `elems` elements.
 constexpr long dx_max_splits(long elems) { return elems <= 1L << 19 ? 8 : elems <= 1L << 22 ? 4 : 1; }
-// Whether blocks may share a contraction (kDxSummed: a sum over slots, which the
-// join takes the place of, would follow anyway).
+// Whether blocks may share a contraction (kDxSummed: fp32 sums are joined anyway, over
+// a token's slots or with what dx holds).
 enum DxSums { kDxOnePiece, kDxJoined, kDxSummed };
 DxPlan moe_dx_plan(int dtype, const MoeArgs& a, long P, DxSums sums);
 hipError_t launch_moe_dx(int dtype, DxPlan plan, const MoeArgs& a, long P, hipStream_t stream);
 struct DxJoinArgs {
-  const float* part;          // [splits][pairs][d]
+  const float* part;          // [splits][pairs][d] fp32
   const int32_t* pair_row;
   void* out;                  // [pairs / k][d]
   long pairs;
@@ -160,8 +160,8 @@ struct CombineArgs {
   const void* y;              // [T*k][d]
   const int32_t* pair_row;    // [T*k], negative where the pair was dropped
   const float* pair_w;        // [T*k] or null (weight 1)
-  void* out;                  // [T][d], written (accumulate: added to)
-  int32_t k, d, accumulate;
+  void* out;                  // [T][d], written
+  int32_t k, d;
   FastDiv per_row;            // pieces of a row (set by the launcher)
   uint32_t pieces;
 };

@@ -362,11 +362,13 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   const bool rows_are_tokens = im == ACE_INPUT_SHARED && k == 1 && !accumulate;
   const bool summed = pair_rows && !rows_are_tokens;
   const DxPlan plan = moe_dx_plan(dtype, a, P, !ws ? kDxOnePiece : summed ? kDxSummed : kDxJoined);
+  const bool join = summed || plan.splits > 1;   // fp32 sums; the result is rounded once
   a.splits = plan.splits;
-  a.part = static_cast<float*>(ws);
-  a.y = summed ? ws : dx;
+  a.part = join ? static_cast<float*>(ws) : nullptr;
+  a.y = dx;
   hipError_t e = launch_moe_dx(dtype, plan, a, P, st);
-  if (e == hipSuccess && a.splits > 1) {
+  if (e != hipSuccess) return hip_status(e, "input gradient launch");
+  if (join) {
     DxJoinArgs j{};
     j.part = a.part;
     j.pair_row = ert->pair_row;
@@ -379,19 +381,8 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
     j.keep = im == ACE_INPUT_PER_PAIR;
     return hip_status(launch_moe_dx_join(dtype, j, st), "input gradient join launch");
   }
-  if (e == hipSuccess && rows_are_tokens)
-    return hip_status(launch_zero_dropped(dtype, ert->pair_row, T, d_in, dx, st), "input gradient launch");
-  if (e != hipSuccess || !pair_rows) return hip_status(e, "input gradient launch");
-  // the token's rows, or (per pair) each row as a token of its own
-  CombineArgs c{};
-  c.y = ws;
-  c.pair_row = ert->pair_row;
-  c.out = dx;
-  c.k = im == ACE_INPUT_SHARED ? k : 1;
-  c.d = d_in;
-  c.accumulate = accumulate;
-  return hip_status(launch_combine_fwd(dtype, c, im == ACE_INPUT_SHARED ? T : T * k, st),
-                    "input gradient sum launch");
+  if (rows_are_tokens) e = launch_zero_dropped(dtype, ert->pair_row, T, d_in, dx, st);
+  return hip_status(e, "input gradient launch");
 }
 
 // Validation of the combine calls up to their pointers.

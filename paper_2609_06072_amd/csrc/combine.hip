@@ -30,7 +30,6 @@ __global__ __launch_bounds__(kThreads) void combine_fwd_kernel(CombineArgs a) {
   float acc[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.f;
-  bool routed = false;
   for (int j0 = 0; j0 < a.k; j0 += G) {
     int row[G];
     float w[G];
@@ -47,19 +46,11 @@ __global__ __launch_bounds__(kThreads) void combine_fwd_kernel(CombineArgs a) {
     for (int g = 0; g < G; ++g) {
       asm volatile("" : "+v"(f[g]));   // loaded above, not behind the branch
       if (j0 + g >= a.k || row[g] < 0) continue;
-      routed = true;
       float v[PER];
       Tr<T>::to_f32(f[g], v);
 #pragma unroll
       for (int i = 0; i < PER; ++i) acc[i] += w[g] * v[i];
     }
-  }
-  if (a.accumulate) {
-    if (!routed) return;   // (a sum with 0 would lose a zero's sign)
-    float v[PER];
-    Tr<T>::to_f32(Tr<T>::load(out), v);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) acc[i] += v[i];
   }
   Tr<T>::store_nt(out, Tr<T>::from_f32(acc));
 }

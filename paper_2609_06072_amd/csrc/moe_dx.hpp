@@ -17,7 +17,9 @@
 // of the XCD's CUs or fewer, its tiles are cut into two or four column parts, which
 // as many blocks of a second set (launched behind the first) take.  With splits,
 // that many blocks share a tile's contraction (a tile below is then one of these
-// parts) and store fp32 sums for moe_dx_join_kernel.
+// parts).  Where a sum follows (of these parts, of a token's slots, with what dx
+// holds) the fp32 sums go to a.part as they are, for moe_dx_join_kernel, so that a
+// result is rounded once.
 // 8192 x 8192 with a contraction of 1024 131 us, of 2048 228 us (the library's dense
 // products of these sizes 129 and 220): 1.44 us a stage on a full card, 1.24 for a
 // block alone, of which the matrix units are busy for 0.9, and 8 us a tile for its
@@ -344,8 +346,7 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
     // columns 4 g .. 4 g + 3 of a 16-column block of row c16.  Of two neighbouring
     // blocks the lanes of a row trade their 8-byte pieces until lane g holds the
     // 16 bytes g: a store covers 64 bytes of each of 16 rows (32 bytes of them:
-    // 35 us more for 134 MB of results).
-    // With splits the fp32 sums go out as they are.
+    // 35 us more for 134 MB of results).  fp32 sums go out as they are.
     // full: all 32 stores are issued, in a straight line, so that the compiler can
     // count them where it waits for the loads above, which are older.
     // (the lane's number anew: kept, it and what follows from it would be spilled,
@@ -361,7 +362,7 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
 #pragma unroll
       for (int nb = 0; nb < NB; nb += 2) o[nb / 2] = trade4(acc[nb][mb], acc[nb + 1][mb]);
       const int p = __shfl(pc[mb >> 2], 16 * (mb & 3) + lc16, 64);
-      if (!FULL && a.splits > 1) {
+      if (!FULL && a.part) {
         if (row0 + 16 * mb < cur.hi) {
           float* row = a.part + ((size_t)cur.split * a.pairs + p) * N + col1;
 #pragma unroll
@@ -377,7 +378,7 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
-    drained = NB == 8 && a.splits == 1 && cur.u0 + C::BM <= cur.hi && cur.n0 + C::BN <= N;
+    drained = NB == 8 && !a.part && cur.u0 + C::BM <= cur.hi && cur.n0 + C::BN <= N;
     if (drained) {
 #pragma unroll
       for (int mb = 0; mb < 8; ++mb) store(Yes{}, mb);
@@ -442,8 +443,8 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_dx_large_kernel(MoeArgs
 // 4, ..., each through a ring of its own in LDS (the K-block's W rows and the same
 // columns of the x rows), so no barrier stands in the loop; the four sums meet in
 // LDS at the end, in wave order.  Where even the smallest tiles leave CUs idle,
-// several blocks share a tile's K-blocks in the same way (a.splits) and write fp32
-// sums that moe_dx_join_kernel adds, in order.  A third buffer per wave gained nothing (fewer
+// several blocks share a tile's K-blocks in the same way (a.splits) and moe_dx_join_kernel
+// adds their sums, in order.  A third buffer per wave gained nothing (fewer
 // streams at a time serve HBM better).  64 experts of 2048 x 1024 with 4 rows
 // each: 44 us, 5.9 TB/s of weights.
 template <typename T, int NRB, int BN_>
@@ -580,15 +581,18 @@ __global__ __launch_bounds__(256) void moe_dx_stream_kernel(MoeArgs a) {
     for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * C::BM + row) * C::CST + col);
     if (u0 + row < u_end && n0 + col < N) {
       const size_t at = (size_t)a.pair_list[u0 + row] * N + n0 + col;
-      if (a.splits > 1) *reinterpret_cast<f32x4*>(a.part + (size_t)split * a.pairs * N + at) = v;
+      if (a.part) *reinterpret_cast<f32x4*>(a.part + (size_t)split * a.pairs * N + at) = v;
       else *reinterpret_cast<T4*>(Y + at) = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
     }
   }
 }
 
-// dx (four columns per thread) from the sums of the splits: of one pair, or of a
-// token's routed slots in slot order.
-template <typename T>
+// dx (four columns per thread) from the fp32 sums of the splits: of one pair, or of a
+// token's routed slots in slot order, added to what dx holds where accumulate asks for
+// it, and rounded once.
+// The loads of G sums are under way at a time, without branches between them (one
+// token, 8 experts of 2048 x 1024: the call 16.3 -> 13.0 us).
+template <typename T, int G>
 __global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
   typedef __attribute__((ext_vector_type(4))) T T4;
   const uint32_t idx = blockIdx.x * kThreads + threadIdx.x;
@@ -596,9 +600,6 @@ __global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
   const uint32_t t = a.per_row.div(idx), col = 4 * (idx - t * a.per_row.d);
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   bool routed = false;
-  // the loads of eight sums under way at a time, without branches between them
-  // (one token, 8 experts of 2048 x 1024: the call 16.3 -> 13.0 us)
-  constexpr int G = 8;
   const int n = a.k * a.splits;
   for (int i0 = 0, j = 0, s = 0; i0 < n; i0 += G) {
     int row[G];
@@ -607,7 +608,7 @@ __global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
     for (int g = 0; g < G; ++g) {
       const size_t p = (size_t)t * a.k + j;
       row[g] = a.pair_row[p];
-      f[g] = *reinterpret_cast<const f32x4*>(a.part + ((size_t)s * a.pairs + p) * a.d + col);
+      f[g] = Tr<float>::load_nt(a.part + ((size_t)s * a.pairs + p) * a.d + col);
       if (i0 + g + 1 < n && ++s == a.splits) {
         s = 0;
         ++j;
@@ -627,14 +628,23 @@ __global__ __launch_bounds__(kThreads) void moe_dx_join_kernel(DxJoinArgs a) {
     const T4 o = *out;
     v += f32x4{(float)o[0], (float)o[1], (float)o[2], (float)o[3]};
   }
-  *out = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+  __builtin_nontemporal_store(T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}, out);
+}
+
+// Sums under way: as many as there are, up to eight.
+template <typename T>
+void moe_dx_join(const DxJoinArgs& a, unsigned grid, hipStream_t stream) {
+  const int n = a.k * a.splits;
+  if (n == 1) moe_dx_join_kernel<T, 1><<<grid, kThreads, 0, stream>>>(a);
+  else if (n == 2) moe_dx_join_kernel<T, 2><<<grid, kThreads, 0, stream>>>(a);
+  else if (n <= 4) moe_dx_join_kernel<T, 4><<<grid, kThreads, 0, stream>>>(a);
+  else moe_dx_join_kernel<T, 8><<<grid, kThreads, 0, stream>>>(a);
 }
 
 // ---- tiles of 128 rows x 128 columns, four waves of 64 x 64, one K-block a stage
 // in a ring in LDS, several blocks per CU (while one waits or stores, the others use
 // the matrix units): fp32 with many rows per expert, bf16 where the large tiles leave
-// CUs idle.  Tile order as in the large tiles; with splits, that many blocks share a
-// tile's K-blocks and store fp32 sums for moe_dx_join_kernel.
+// CUs idle.  Tile order, splits and fp32 sums as in the large tiles.
 template <typename T>
 struct DxTile {
   static constexpr int KB = Tr<T>::KB, BM = 128, BN = 128, NBUF = sizeof(T) == 4 ? 3 : 4, PER_CU = sizeof(T) == 4 ? 3 : 2;
@@ -735,8 +745,8 @@ __global__ __launch_bounds__(256, DxTile<T>::PER_CU) void moe_dx_tile_kernel(Moe
   for (int mb = 0; mb < 4; ++mb) {
     const int u = u0 + 64 * wy + 16 * mb + c16;
     const size_t at = (size_t)a.pair_list[min(u, hi - 1)] * N;
-    if (sizeof(T) == 4 || a.splits > 1) {
-      float* row = (a.splits > 1 ? a.part + (size_t)split * a.pairs * N : reinterpret_cast<float*>(Y)) + at + col0;
+    if (sizeof(T) == 4 || a.part) {
+      float* row = (a.part ? a.part + (size_t)split * a.pairs * N : reinterpret_cast<float*>(Y)) + at + col0;
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb)
         if (u < hi && col0 + 16 * nb < N) *reinterpret_cast<f32x4*>(row + 16 * nb) = acc[nb][mb];

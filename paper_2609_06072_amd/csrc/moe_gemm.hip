@@ -1092,8 +1092,8 @@ hipError_t launch_moe_dx_join(int dtype, DxJoinArgs a, hipStream_t stream) {
   a.per_row = FastDiv(a.d / 4);
   a.pieces = (uint32_t)(a.pairs / a.k * (a.d / 4));
   const unsigned grid = (a.pieces + kThreads - 1) / kThreads;
-  if (dtype == ACE_BF16) moe_dx_join_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a);
-  else moe_dx_join_kernel<float><<<grid, kThreads, 0, stream>>>(a);
+  if (dtype == ACE_BF16) moe_dx_join<__bf16>(a, grid, stream);
+  else moe_dx_join<float>(a, grid, stream);
   return hipGetLastError();
 }
 
