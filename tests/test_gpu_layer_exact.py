@@ -75,3 +75,36 @@ def check(ace, T, k, E, d_in, d_out, ids, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sums_are_rounded_once(ace, T, k, E, d_in, d_out, dtype):
     check(ace, T, k, E, d_in, d_out, D.routing("random", T, k, E), dtype)
+
+
+@pytest.mark.parametrize("form", D.FORMS, ids=lambda f: "x".join(map(str, f[:5])))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_forms(ace, form, dtype):
+    T, k, E, d_in, d_out, kind = form[:6]
+    check(ace, T, k, E, d_in, d_out, D.routing(kind, T, k, E), dtype)
+
+
+@pytest.mark.parametrize("form", [f for f in D.FORMS if f[6] == D.LARGE and f[8] >= 2 and f[4] % (128 * f[7])][:6],
+                         ids=lambda f: "x".join(map(str, f[:5])))
+def test_infinities_between_tiles(ace, form):
+    """Blocks of several large tiles with a ragged contraction: infinities and NaN at
+    its end reach the pairs that use them, not those of the tiles before and after."""
+    T, k, E, d_in, d_out, kind = form[:6]
+    ids = D.routing(kind, T, k, E)
+    rt = ace.ace_group_permute(torch.from_numpy(ids).cuda(), E, None, E, ace.ACE_ROWS_EXPERT)
+    dy, W = whole(2, T * k, d_out, dtype="bf16"), whole(3, E, d_out, d_in, dtype="bf16")
+    rows = exact_rows(dy, W, ids, E)
+    W[E // 2, d_out - 1, :] = float("nan")
+    W[E // 4, 0, :] = float("inf")
+    dy[7, d_out - 1] = float("inf")
+    dy[T * k // 2, :8] = float("nan")
+    dx = torch.zeros(T * k, d_in, dtype=torch.bfloat16, device="cuda")
+    n = ace.ace_workspace_bytes(ace.ACE_OP_MOE_DX, T, k, d_in, d_out, E, 0)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    ace.ace_moe_dx(dy, W, rt, dx, input_mode=ace.ACE_INPUT_PER_PAIR, ws=ws)
+    ok = L.routed(ids, E).reshape(-1)
+    hit = np.isin(ids.reshape(-1), (E // 2, E // 4)) & ok
+    hit[[7, T * k // 2]] |= ok[[7, T * k // 2]]
+    hit = torch.from_numpy(hit).cuda()
+    assert not bool(torch.isfinite(dx[hit]).any())
+    same("the other rows", dx[~hit], rows[~hit])
