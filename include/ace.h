@@ -332,8 +332,9 @@ ace_status ace_moe_lora_fwd(ace_dtype dtype, ace_input_mode input_mode, int32_t 
  *               where it holds an fp32 row per pair (a token's rows are added in
  *               slot order, then to dx where accumulate asks for it, all in fp32,
  *               and the result is rounded once), in calls of few tiles one for
- *               each of the blocks that share a contraction.  May be NULL for the
- *               per-pair input with accumulate = 0: then no contraction is
+ *               each of the blocks that share a contraction.  One that is large
+ *               enough for T, k and d_in is for all smaller ones.  May be NULL
+ *               for the per-pair input with accumulate = 0: then no contraction is
  *               shared.  No initialisation.
  * Limits: T * k * d_out and T * k * d_in below 2^33 - 4096, d_in below 2^24,
  * d_out below 2^30.

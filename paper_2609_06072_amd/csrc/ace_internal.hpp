@@ -137,7 +137,15 @@ struct DxPlan {
   int splits;   // blocks that share a tile's contraction
 };
 // At most so many for a result of `elems` elements.
-constexpr long dx_max_splits(long elems) { return elems <= 1L << 19 ? 8 : elems <= 1L << 22 ? 4 : 1; }
+constexpr long kDxElems8 = 1L << 19, kDxElems4 = 1L << 22;
+constexpr long dx_max_splits(long elems) { return elems <= kDxElems8 ? 8 : elems <= kDxElems4 ? 4 : 1; }
+// fp32 sums of a call of `elems` elements and of every smaller one, whose contractions
+// more blocks may share.
+constexpr long dx_max_sums(long elems) {
+  const long by4 = 4 * (elems < kDxElems4 ? elems : kDxElems4), by8 = 8 * (elems < kDxElems8 ? elems : kDxElems8);
+  const long shared = by4 > by8 ? by4 : by8;
+  return elems > shared ? elems : shared;
+}
 // Whether blocks may share a contraction (kDxSummed: fp32 sums are joined anyway, over
 // a token's slots or with what dx holds).
 enum DxSums { kDxOnePiece, kDxJoined, kDxSummed };

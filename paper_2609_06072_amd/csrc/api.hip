@@ -297,8 +297,7 @@ ace_status check_rows(ace_dtype dtype, int32_t d) {
 constexpr int64_t kMaxRowElems = ((int64_t)1 << 33) - 4096;
 
 size_t moe_dx_ws_bytes(int T, int k, int d_in) {
-  const size_t rows = (size_t)T * k * d_in;
-  return rows * dx_max_splits((long)rows) * sizeof(float);
+  return (size_t)dx_max_sums((long)T * k * d_in) * sizeof(float);
 }
 
 ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, int32_t d_in,

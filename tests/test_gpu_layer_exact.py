@@ -84,6 +84,25 @@ def test_forms(ace, form, dtype):
     check(ace, T, k, E, d_in, d_out, D.routing(kind, T, k, E), dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_workspace_for_smaller_calls(ace, dtype):
+    """Sized for the largest batch, used for smaller ones on both sides of the sizes
+    from which fewer blocks share a contraction."""
+    k, E, d_in, d_out = 1, 4, 2048, 1032
+    n = ace.ace_workspace_bytes(ace.ACE_OP_MOE_DX, 2049, k, d_in, d_out, E, 0)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    W = whole(3, E, d_out, d_in, dtype=dtype)
+    for T in (2049, 2048, 257, 256, 7, 1):
+        ids = D.routing("even", T, k, E)
+        rt = ace.ace_group_permute(torch.from_numpy(ids).cuda(), E, None, E, ace.ACE_ROWS_EXPERT)
+        dy = whole(2, T, d_out, dtype=dtype)
+        rows = exact_rows(dy, W, ids, E)
+        same(T, ace.ace_moe_dx(dy, W, rt, ws=ws), rows)
+        acc = torch.ones(T, d_in, dtype=DT[dtype], device="cuda")
+        ace.ace_moe_dx(dy, W, rt, acc, input_mode=ace.ACE_INPUT_PER_PAIR, accumulate=True, ws=ws)
+        same(T, acc, rows + 1)
+
+
 @pytest.mark.parametrize("form", [f for f in D.FORMS if f[6] == D.LARGE and f[8] >= 2 and f[4] % (128 * f[7])][:6],
                          ids=lambda f: "x".join(map(str, f[:5])))
 def test_infinities_between_tiles(ace, form):
