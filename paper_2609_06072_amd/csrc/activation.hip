@@ -124,6 +124,7 @@ __device__ inline void store_packed(const ace_packed_act& c, const Spot& s, cons
   if (s.first) c.exps[s.block] = (uint8_t)e;
 }
 
+// (for pieces inside the row only)
 template <typename T>
 __device__ inline void load_packed(const ace_packed_act& c, const Spot& s, float* v) {
   decode<T>(*reinterpret_cast<const typename CodeWord<T>::type*>(c.codes + s.elem), c.exps[s.block], v);
@@ -181,6 +182,8 @@ template <typename T, int CKPT>
 __global__ __launch_bounds__(kThreads) void swiglu_fwd_kernel(ActGeom a, SwigluArgs w) {
   constexpr int PER = Tr<T>::PER;
   const Spot s = spot<T>(a, blockIdx.x * kThreads + threadIdx.x);
+  // (writing checkpoints, lanes past the row's end take part in the exchanges)
+  if (CKPT != kWritePacked && !s.in) return;
   float g[PER], u[PER], o[PER];
   load_gu<T, CKPT>(w, s, g, u);
   if (CKPT == kWritePacked) {
