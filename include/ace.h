@@ -403,8 +403,9 @@ ace_status ace_act_unpack(ace_dtype dtype, int64_t rows, int32_t d, const ace_pa
  * SwiGLU between the gate/up and the down projections of an expert:
  *   a  = g sigma(g) u,             sigma(g) = 1 / (1 + e^-g)
  *   dg = da u sigma(g) (1 + g (1 - sigma(g))),   du = da g sigma(g)
- * for every row (in fp32, each result rounded once; rows of dropped pairs give
- * whatever their inputs make of them).
+ * for every row (in fp32, each result rounded once, da u formed first; rows of
+ * dropped pairs give whatever their inputs make of them).  sigma is held to 2^-252,
+ * past fp32's smallest numbers, and is 0 below (g < -174.6).
  *   rows, d     as for ace_act_pack.
  *   g, u, da    device [rows, d], dtype, 16-byte aligned.
  *   a, dg, du   device [rows, d], dtype, 16-byte aligned: written.

@@ -19,6 +19,8 @@
 // neighbouring lanes: its largest |x| comes from two or three lane exchanges,
 // without LDS.  Rows are filled up to whole blocks (lanes past the row's end
 // hold zeros and store nothing).
+#include <type_traits>
+
 #include "ace_device.hpp"
 #include "ace_internal.hpp"
 
@@ -147,21 +149,43 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(ActGeom a, ace_packed_
   store_piece<T>(x, s, v);
 }
 
-// sigma(g) and 1 - sigma(g) without overflow or cancellation: with
+// sigma(g) = sig * scale^2 and 1 - sigma(g) without overflow or cancellation: with
 // t = exp(-|g|), one of them is 1 / (1 + t) and the other t / (1 + t).
 // t = 2^n e^(r ln 2): n the product of |g| and -log2 e as rounded and r, its error
 // and that of the constant, to first order; with the hardware's 2^n and reciprocal
 // (1 ulp each) t is within 2 ulp.  (expf and a division bound the passes that read
 // 8-bit codes: a from checkpoints of 32768 x 1408 47.7 us.)
-__device__ inline void sigmoid2(float g, float& sig, float& one_minus) {
+// The hardware's 2^n is 0 below the normal numbers, where sigma u or sigma da need
+// not be small.  FAR, for rows with g below kFar: below n = -100 it gives 2^(n + 126)
+// (exact: n + 126 is), and scale 2^-63 goes once into the other factor and once into
+// the product, so that neither leaves the range while the result is in it.  1 + t is
+// 1 there.  sigma below 2^-252 (g < -174.6) is 0.  (FAR for all rows: the three passes
+// over 32768 x 1408 with checkpoints 150 -> 158 us.)
+constexpr float kFar = -69.f;   // n > -100
+
+template <bool FAR>
+__device__ inline void sigmoid2(float g, float& sig, float& one_minus, float& scale) {
+#pragma clang fp contract(off)   // (n + 126 of n as rounded, or r is not its error)
   constexpr float kLog2e = 1.44269502f, kLog2eLow = 1.92596303e-8f;   // log2 e in two parts
   const float x = fminf(fabsf(g), 200.f);   // (e^-200 is 0; an infinity has no r)
   const float n = x * -kLog2e;
+  const bool far = FAR && n < -100.f;
   const float r = fmaf(x, -kLog2eLow, fmaf(x, -kLog2e, -n));
-  const float e = __builtin_amdgcn_exp2f(n);
-  const float t = fmaf(e, r * 0.693147181f, e), p = __builtin_amdgcn_rcpf(1.f + t), q = t * p;
+  const float e = __builtin_amdgcn_exp2f(far ? n + 126.f : n);
+  const float t = fmaf(e, r * 0.693147181f, e), p = far ? 1.f : __builtin_amdgcn_rcpf(1.f + t), q = t * p;
   sig = g < 0.f ? q : p;
-  one_minus = g < 0.f ? p : q;
+  one_minus = g < 0.f ? p : far ? 0.f : q;
+  scale = far && g < 0.f ? 0x1p-63f : 1.f;
+}
+
+// Calls f with whether any of a thread's g is below kFar.
+template <int PER, typename F>
+__device__ inline void by_range(const float* g, const F& f) {
+  float least = g[0];
+#pragma unroll
+  for (int i = 1; i < PER; ++i) least = fminf(least, g[i]);
+  if (least < kFar) f(std::true_type{});
+  else f(std::false_type{});
 }
 
 // Where g and u come from, and whether their checkpoints are written.
@@ -191,12 +215,14 @@ __global__ __launch_bounds__(kThreads) void swiglu_fwd_kernel(ActGeom a, SwigluA
     store_packed<T>(w.u8, s, u);
   }
   if (!s.in) return;
+  by_range<PER>(g, [&](auto far) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    float sig, rest;
-    sigmoid2(g[i], sig, rest);
-    o[i] = g[i] * sig * u[i];
-  }
+    for (int i = 0; i < PER; ++i) {
+      float sig, rest, scale;
+      sigmoid2<far>(g[i], sig, rest, scale);
+      o[i] = g[i] * sig * (u[i] * scale) * scale;
+    }
+  });
   store_piece<T>(w.a, s, o);
 }
 
@@ -208,13 +234,15 @@ __global__ __launch_bounds__(kThreads) void swiglu_bwd_kernel(ActGeom a, SwigluA
   float da[PER], g[PER], u[PER], dg[PER], du[PER];
   load_piece<T>(w.da, s, da);
   load_gu<T, CKPT>(w, s, g, u);
+  by_range<PER>(g, [&](auto far) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    float sig, rest;
-    sigmoid2(g[i], sig, rest);
-    dg[i] = da[i] * u[i] * (sig * (1.f + g[i] * rest));
-    du[i] = da[i] * (g[i] * sig);
-  }
+    for (int i = 0; i < PER; ++i) {
+      float sig, rest, scale;
+      sigmoid2<far>(g[i], sig, rest, scale);
+      dg[i] = da[i] * u[i] * scale * (sig * (1.f + g[i] * rest)) * scale;
+      du[i] = da[i] * scale * (g[i] * sig) * scale;
+    }
+  });
   store_piece<T>(w.dg, s, dg);
   store_piece<T>(w.du, s, du);
 }
