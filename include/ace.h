@@ -321,7 +321,7 @@ ace_status ace_moe_lora_fwd(ace_dtype dtype, ace_input_mode input_mode, int32_t 
  *   dy          device [T*k, d_out], dtype; rows of dropped pairs are not used.
  *   W           device [E, d_out, d_in], dtype, as for ace_moe_lora_fwd.
  *   expert_rt   rows from ace_group_permute in ACE_ROWS_EXPERT mode over E
- *               experts.
+ *               experts; offsets, pair_row and pair_list are read.
  *   accumulate  0: dx is written; 1: dx += (gate and up share their input).
  *   dx          device, [T, d_in] (shared) or [T*k, d_in] (per pair), dtype.
  *               Per pair, rows of dropped pairs are left untouched; shared, a

@@ -323,7 +323,7 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   if ((int64_t)T * k * d_out >= kMaxRowElems || (int64_t)T * k * d_in >= kMaxRowElems)
     return fail(ACE_ERR_UNSUPPORTED, "T*k*d_out or T*k*d_in reaches 2^33 elements");
   if (accumulate != 0 && accumulate != 1) return fail(ACE_ERR_INVALID_ARG, "accumulate = %d", accumulate);
-  if (!ert || !ert->offsets || (T > 0 && (!ert->row_token || !ert->row_slots || !ert->pair_row || !ert->pair_list)))
+  if (!ert || !ert->offsets || (T > 0 && (!ert->pair_row || !ert->pair_list)))
     return fail(ACE_ERR_INVALID_ARG, "expert routing is NULL");
   if (ert->mode != ACE_ROWS_EXPERT || ert->n_keys != E)
     return fail(ACE_ERR_INVALID_ARG, "expert_rt must be ACE_ROWS_EXPERT routing over %d experts", E);
@@ -347,8 +347,6 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
   a.x = dy;
   a.W = W;
   a.offsets = ert->offsets;
-  a.row_token = ert->row_token;
-  a.row_slots = ert->row_slots;
   a.pair_list = ert->pair_list;
   a.E = E;
   a.k = k;

@@ -127,3 +127,14 @@ def test_infinities_between_tiles(ace, form):
     hit = torch.from_numpy(hit).cuda()
     assert not bool(torch.isfinite(dx[hit]).any())
     same("the other rows", dx[~hit], rows[~hit])
+
+
+def test_reads_no_more_of_the_routing_than_it_needs(ace):
+    """The rows' tokens and slots, which these kernels do not use, may be absent."""
+    T, k, E, d_in, d_out = 300, 2, 4, 520, 328
+    ids = D.routing("random", T, k, E)
+    rt = ace.ace_group_permute(torch.from_numpy(ids).cuda(), E, None, E, ace.ACE_ROWS_EXPERT)
+    dy, W = whole(2, T * k, d_out, dtype="bf16"), whole(3, E, d_out, d_in, dtype="bf16")
+    want = ace.ace_moe_dx(dy, W, rt)
+    rt.c.row_token = rt.c.row_slots = None
+    same("without", ace.ace_moe_dx(dy, W, rt), want)
