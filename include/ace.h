@@ -362,7 +362,8 @@ ace_status ace_moe_dx(ace_dtype dtype, ace_input_mode input_mode, int32_t T, int
  *               untouched.  May be y itself.
  *   dw          device fp32 [T, k] or NULL: written (0 for dropped pairs).
  * d must be a multiple of 8 (bf16) or 4 (f32); y, out, dout and dy 16-byte
- * aligned.  T * k * d below 2^33 - 4096.  Deterministic.
+ * aligned; out must not overlap y, nor dy dout, unless k = 1.  T * k * d below
+ * 2^33 - 4096.  Deterministic.
  */
 ace_status ace_moe_combine_fwd(ace_dtype dtype, int32_t T, int32_t k, int32_t d, const void* y,
                                const float* pair_w, const ace_routing* rt, void* out,
@@ -415,7 +416,8 @@ ace_status ace_act_unpack(ace_dtype dtype, int64_t rows, int32_t d, const ace_pa
  *               backward).  A forward that is given g and u writes their
  *               checkpoints in the same pass; a backward takes one or the other.
  * An output may be the same buffer as an input that has its type and shape
- * (dg = g, du = u, a = g, ...); other overlaps are not allowed.
+ * (dg = g, du = u, a = g, ...); other overlaps are not allowed, two outputs in
+ * one buffer among them.
  */
 ace_status ace_swiglu_fwd(ace_dtype dtype, int64_t rows, int32_t d, const void* g, const void* u,
                           void* a, const ace_packed_act* g_packed, const ace_packed_act* u_packed,

@@ -342,6 +342,9 @@ ace_status run_moe_dx(ace_dtype dtype, ace_input_mode im, int32_t T, int32_t k, 
     if (!aligned(ws, 256)) return fail(ACE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   }
   if (T == 0) return ok();
+  if (dx == dy || dx == W) return fail(ACE_ERR_INVALID_ARG, "dx must not overlap dy or W");
+  if (ws && (ws == dx || ws == dy || ws == W))
+    return fail(ACE_ERR_INVALID_ARG, "the workspace must not overlap dy, W or dx");
   const hipStream_t st = static_cast<hipStream_t>(stream);
   MoeArgs a{};
   a.x = dy;
@@ -452,6 +455,9 @@ ace_status run_swiglu(bool bwd, ace_dtype dtype, int64_t rows, int32_t d, const 
     return s;
   }
   if (rows == 0) return ok();
+  if (bwd && dg == du) return fail(ACE_ERR_INVALID_ARG, "dg and du must not overlap");
+  if (!bwd && g8 && !held && (g8->codes == u8->codes || g8->exps == u8->exps))
+    return fail(ACE_ERR_INVALID_ARG, "g_packed and u_packed must not overlap");
   w.da = da;
   w.g = g;
   w.u = u;
@@ -628,6 +634,7 @@ ace_status ace_moe_combine_fwd(ace_dtype dtype, int32_t T, int32_t k, int32_t d,
   if (!aligned(y, 16) || !aligned(out, 16))
     return fail(ACE_ERR_INVALID_ARG, "y and out must be 16-byte aligned");
   if (T == 0) return ok();
+  if (k > 1 && out == y) return fail(ACE_ERR_INVALID_ARG, "out must not overlap y");
   CombineArgs c{};
   c.y = y;
   c.pair_row = rt->pair_row;
@@ -649,6 +656,7 @@ ace_status ace_moe_combine_bwd(ace_dtype dtype, int32_t T, int32_t k, int32_t d,
     return fail(ACE_ERR_INVALID_ARG, "dout, y and dy must be 16-byte aligned");
   if (!aligned(dw, 4)) return fail(ACE_ERR_INVALID_ARG, "dw misaligned");
   if (T == 0) return ok();
+  if (k > 1 && dy == dout) return fail(ACE_ERR_INVALID_ARG, "dy must not overlap dout");
   CombineBwdArgs c{};
   c.dout = dout;
   c.y = y;
