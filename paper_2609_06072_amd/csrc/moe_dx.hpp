@@ -1,5 +1,5 @@
-// Input gradient of the expert projection, many rows per expert (part of
-// moe_gemm.hip): y[p] = W_e^T x[p] per pair, W_e [K][N] row-major, so the
+// Input gradient of the expert projection, many rows per expert (included by
+// moe_gemm.hip behind what both share): y[p] = W_e^T x[p] per pair, W_e [K][N] row-major, so the
 // contraction runs over W_e's rows.
 //
 // bf16, tiles of 256 rows x 256 columns, four waves of 128 x 128 as in
@@ -24,6 +24,10 @@
 // products of these sizes 129 and 220): 1.44 us a stage on a full card, 1.24 for a
 // block alone, of which the matrix units are busy for 0.9, and 8 us a tile for its
 // results and the next one's start.
+#pragma once
+
+namespace ace {
+namespace {
 
 // Chunk swizzle of a 128-byte W^T row: pairs of chunks trade places, so that the
 // 32 bytes that a transposed read takes of the rows 8 g + (0..3) (+ 4) spread
@@ -759,3 +763,6 @@ __global__ __launch_bounds__(256, DxTile<T>::PER_CU) void moe_dx_tile_kernel(Moe
     }
   }
 }
+
+}  // namespace
+}  // namespace ace

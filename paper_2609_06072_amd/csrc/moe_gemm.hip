@@ -642,7 +642,13 @@ __global__ __launch_bounds__(Large::THREADS, 1) void moe_gemm_large_kernel(MoeAr
   }
 }
 
+}  // namespace
+}  // namespace ace
+
 #include "moe_dx.hpp"
+
+namespace ace {
+namespace {
 
 // ---------------------------------------------------------------- few rows per expert
 //
