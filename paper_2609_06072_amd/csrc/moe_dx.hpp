@@ -287,7 +287,8 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
   // The copies come to the end of the tile in its last stage but two, an odd one.
   // drained: the first four half-steps behind a tile whose 32 stores were all
   // issued.  The slots they read were copied before the stores, which may all be
-  // under way beside the 24 copies behind the needed ones.
+  // under way beside the 24 copies behind the needed ones.  (As compiled they have
+  // ended by then: set_tile reloads spilled chunk numbers, behind all of them.)
   auto half = [&](auto par_c, auto mma_c, auto odd_c, bool drained, F (&x1)[4], F (&wc)[16], F (&x1n)[4], F (&wn)[16]) {
     constexpr int PAR = decltype(par_c)::value;
     constexpr bool MMA = decltype(mma_c)::value;
@@ -353,8 +354,8 @@ __device__ inline void moe_dx_large_block(const MoeArgs& a, char* smem, int befo
     // 35 us more for 134 MB of results).  fp32 sums go out as they are.
     // full: all 32 stores are issued, in a straight line, so that the compiler can
     // count them where it waits for the loads above, which are older.
-    // (the lane's number anew: kept, it and what follows from it would be spilled,
-    // and a reload waits for the copies in flight)
+    // (the lane's number anew: kept, it and what follows from it would be spilled
+    // too)
     const int ln = lane_id(), lc16 = ln & 15, lg = ln >> 4;
     const int col0 = cur.n0 + CW * wx + 8 * lg, col1 = cur.n0 + CW * wx + 4 * lg, row0 = cur.u0 + 128 * wy + lc16;
     auto store = [&](auto full_c, int mb) {
