@@ -956,16 +956,16 @@ long dx_blocks(const MoeArgs& a, long P, long bm, long bn) {
 //   5032, 456, 16           200    79 /  93       444   137 /  99
 //   1568, 424, 4            981    23 /  32      2000    42 /  35
 //   512, 256, 8             500    10 /  12      1000    16 /  13
-// Best of the above / 128 x 128 (in one, or * two blocks a contraction):
-//   1440, 1504, 4           578    42 /  32         3456, 272, 16    1104    87 /  74
-//   1032, 1320, 8           322    32 /  25         2200, 288, 32     595    69 /  60
-//   2048, 1024, 64           64    74 /  65         2336, 1544, 8      75    34 /  27 *
-//   4096, 4096, 8            64    77 /  65          264, 496, 96      75    22 /  17
-//   1024, 2048, 64          512   192 / 258          616, 1560, 128   214   128 / 162
-// Large tiles, one block for a contraction / as many as estimated best:
-//   7784, 912, 16           164   178 / 121
-//   6728, 568, 32           147   151 / 125
-//   5624, 336, 64           130   125 / 113
+// Best of the above / 128 x 128 (in one, or * two blocks a contraction), shared input:
+//   1440, 1504, 4           578    36 /  33         3456, 272, 16    1104    94 /  76
+//   1032, 1320, 8           322    32 /  31         2200, 288, 32     595    81 /  68
+//   2048, 1024, 64           64    77 /  67         2336, 1544, 8      75    35 /  28 *
+//   4096, 4096, 8            64    80 /  70          264, 496, 96      75    24 /  20
+//   1024, 2048, 64          512   229 / 307          616, 1560, 128   214   155 / 197
+// Large tiles, one block for a contraction / as many as estimated best, shared input:
+//   7784, 912, 16           164   140 /  98
+//   6728, 568, 32           147   146 / 113
+//   5624, 336, 64           130   125 / 101
 // Among the streaming forms (32 x 64 / 64 x 64 / 32 x 128 / 64 x 128), the first
 // that fits the CUs once, and 128 columns beyond:
 //   1568, 424, 4             20    13 /  13 /  17 /  18     300    26 /  19 /  17 /  21
@@ -985,16 +985,16 @@ constexpr long kDxStream32 = 20, kDxShortK = 640, kDxShort32 = 80;
 // Blocks per tile of the narrow forms: as many as fill the chip once (fp32, whose
 // matrix work is longer: twice), each with 320 of the contraction at least, in bf16
 // 640 where the join does not take the place of the sum over slots (460 pairs of 496
-// x 608, 4 experts: 10.1 us a call, in two 12.2).
+// x 608, 4 experts, per pair: 6.1 us a call, in two 9.0).
 // us a call, shared input (1 / 2 / 4 / 8 blocks a tile):
-//   bf16  9816 x 544, 4 experts, 16 pairs      46.6 / 28.1 / 18.8 / 18.6
-//         2000 x 304, 8, 240                   18.7 / 13.6 / 11.0 / 11.8
-//         1504 x 1000, 8, 80                   15.3 / 13.4 / 13.6 / 16.5
-//         1024 x 512, 8, 512                   10.8 / 11.6 / 12.3 / 17.4
-//   fp32  4952 x 296, 64, 6                    50.5 / 29.3 / 18.5 / 13.4
-//         1568 x 424, 4, 200                   28.0 / 18.7 / 13.9 / 16.0
-//         1024 x 512, 8, 512                   20.9 / 19.9 / 18.5 / 20.9
-//         1016 x 1920, 4, 132                  20.5 / 20.1 / 18.4 / 24.1
+//   bf16  9816 x 544, 4 experts, 16 pairs      46.5 / 28.0 / 18.7 / 18.9
+//         2000 x 304, 8, 240                   18.5 / 13.3 / 11.2 / 11.9
+//         1504 x 1000, 8, 80                   15.4 / 13.3 / 14.0 / 16.8
+//         1024 x 512, 8, 512                   11.3 / 10.9 / 11.8 / 16.6
+//   fp32  4952 x 296, 64, 6                    50.6 / 29.4 / 19.3 / 14.1
+//         1568 x 424, 4, 200                   28.0 / 18.9 / 14.6 / 16.6
+//         1024 x 512, 8, 512                   20.7 / 19.4 / 17.8 / 20.0
+//         1016 x 1920, 4, 132                  20.5 / 19.7 / 18.3 / 21.8
 DxPlan dx_narrow(bool f32, DxKernel kernel, const MoeArgs& a, long P, DxSums sums) {
   const long bm = kernel == kDxS16x64 ? 16 : kernel == kDxS32x64 ? 32 : 64;
   const long fill = (f32 ? 2L : 1L) * device_cu_count() / dx_blocks(a, P, bm, 64);
