@@ -546,6 +546,13 @@ def _alloc(make, stream, *shape, **kw):
         return make(*shape, **kw)
 
 
+def _width(name: str, n: int) -> int:
+    """A row length as the library's 32-bit argument (a longer one would wrap)."""
+    if n >= 1 << 31:
+        raise ValueError(f"{name} has {n} columns, more than 2^31 - 1")
+    return n
+
+
 def _check_routing(routing: Routing, T: int, k: int, index: int) -> None:
     if (routing.c.T, routing.c.k) != (T, k):
         raise ValueError(f"routing was built for T={routing.c.T} k={routing.c.k}, the call has "
@@ -569,6 +576,8 @@ def ace_moe_dx(dy, W, expert_routing: Routing, dx=None, input_mode: int = ACE_IN
     if W.dim() != 3:
         raise ValueError(f"W must be [E, d_out, d_in], got {tuple(W.shape)}")
     E, d_out, d_in = W.shape
+    _width("dx", d_in)
+    _width("dy", d_out)
     dt = W.dtype
     _check_routing(expert_routing, T, k, dev)
     shared = input_mode == ACE_INPUT_SHARED
@@ -597,7 +606,7 @@ def ace_moe_combine_fwd(y, routing: Routing, out=None, pair_w=None, stream=None)
     dev = _on_device(y)
     if y.dim() != 2 or y.shape[0] != T * k:
         raise ValueError(f"y must be [T*k={T * k}, d], got {tuple(y.shape)}")
-    d, dt = y.shape[1], y.dtype
+    d, dt = _width("y", y.shape[1]), y.dtype
     _check_routing(routing, T, k, dev)
     if out is None:
         out = _alloc(torch.empty, stream, T, d, dtype=dt, device=y.device)
@@ -616,7 +625,7 @@ def ace_moe_combine_bwd(dout, routing: Routing, dy=None, pair_w=None, y=None, dw
     dev = _on_device(dout)
     if dout.dim() != 2 or dout.shape[0] != T:
         raise ValueError(f"dout must be [T={T}, d], got {tuple(dout.shape)}")
-    d, dt = dout.shape[1], dout.dtype
+    d, dt = _width("dout", dout.shape[1]), dout.dtype
     _check_routing(routing, T, k, dev)
     if dy is None:
         dy = _alloc(torch.zeros, stream, T * k, d, dtype=dt, device=dout.device)
@@ -654,6 +663,7 @@ def _packed(name: str, c: PackedAct, rows: int, d: int, index: int):
 def _rows(name: str, t: torch.Tensor):
     if t.dim() != 2:
         raise ValueError(f"{name} must be [rows, d], got {tuple(t.shape)}")
+    _width(name, t.shape[1])
     return t.shape
 
 
@@ -673,7 +683,7 @@ def ace_act_unpack(packed: PackedAct, x=None, dtype=None, stream=None) -> torch.
     """The rows that a checkpoint stands for: into x, or a new tensor of dtype
     (bf16 by default; the values are exact in both types)."""
     dev = _on_device(packed.codes)
-    rows, d = packed.rows, packed.d
+    rows, d = packed.rows, _width("packed", packed.d)
     if x is None:
         x = _alloc(torch.empty, stream, rows, d, dtype=dtype or torch.bfloat16,
                    device=packed.codes.device)
