@@ -1,6 +1,6 @@
 // Input gradient of the expert projection, many rows per expert (included by
-// moe_gemm.hip behind what both share): y[p] = W_e^T x[p] per pair, W_e [K][N] row-major, so the
-// contraction runs over W_e's rows.
+// moe_gemm.hip behind what both share): y[p] = W_e^T x[p] per pair, W_e [K][N]
+// row-major, so the contraction runs over W_e's rows.
 //
 // bf16, tiles of 256 rows x 256 columns, four waves of 128 x 128 as in
 // moe_gemm_large_kernel, with its ring of five 32 KB slots and its half-steps.
